@@ -91,8 +91,18 @@ typedef enum qg_format {
 
 typedef enum qg_out_dtype {
     QG_OUT_BF16 = 0,             /* round-to-nearest-even bfloat16 */
-    QG_OUT_F32 = 1               /* IEEE binary32 */
+    QG_OUT_F32 = 1,              /* IEEE binary32 */
+    QG_OUT_FP8 = 2,              /* E4M3 codes, static scale (qg_gemm_fused only) */
+    QG_OUT_NVFP4 = 3             /* E2M1 codes + E4M3 block scales, static scale (qg_gemm_fused only) */
 } qg_out_dtype;
+
+/* Activation functions of qg_gemm_fused. */
+typedef enum qg_activation {
+    QG_ACT_NONE = 0,
+    QG_ACT_SILU = 1,             /* z / (1 + exp(-z)) */
+    QG_ACT_GELU_TANH = 2,        /* z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) */
+    QG_ACT_GELU_ERF = 3          /* z / 2 (1 + erf(z / sqrt 2)) */
+} qg_activation;
 
 /*
  * qg_quantize_act -- dynamic quantization of a bf16 tensor (activations at
@@ -331,6 +341,104 @@ qg_status qg_gemm_quant_nvfp4(qg_format a_fmt, const void *a, const void *a_bloc
                               int64_t m, int64_t n, int64_t k,
                               void *y_codes, void *y_block_scales, int64_t ldy,
                               const float *y_tensor_scale, void *stream);
+
+/*
+ * qg_gemm_fused -- qg_gemm with what a transformer block does to a linear's
+ * output done in the epilogue, in fp32 on the accumulated sums, so that the
+ * product is rounded once and crosses memory once:
+ *   plain  (gated = 0):  y = act(z + bias) + residual,
+ *   gated  (gated = 1):  y = act(z_gate + bias_gate) (z_up + bias_up),
+ * with z = s_a s_w sum_k deq'(a) deq'(w) as in qg_gemm. Paper: Sec. 4,
+ * quantization paragraph (the quantized linears of the transformer's and the
+ * encoder's feed-forward blocks).
+ *   a_fmt ... k   as for qg_gemm (every supported pair), n the columns of y.
+ *                 gated: the packed weight has 2 n rows, row 2 i the gate's and
+ *                 row 2 i + 1 the up projection's row i, quantized as one tensor.
+ *   epilogue      host memory, read before the call returns:
+ *     act             a qg_activation.
+ *     gated           0 or 1.
+ *     bias            [n] (gated: [2 n], in the order of the weight's rows) of
+ *                     bias_dtype (bf16 or fp32, aligned to an element), or NULL.
+ *     residual        [m, ldr] of residual_dtype (bf16 or fp32, aligned to an
+ *                     element; ldr >= n), or NULL; gated: NULL.
+ *                     It may be y itself (the same pointer, type and pitch:
+ *                     a residual stream updated in place); no other overlap.
+ *   y             out: [m, ldy] of y_dtype: bf16, fp32, FP8 codes, or NVFP4 codes
+ *                 (rows of ldy/2 bytes, 4-byte aligned, ldy % 16 == 0; not for
+ *                 weight-only pairs: QG_ERR_UNSUPPORTED).
+ *   y_block_scales  out, NVFP4 only (else NULL): rows of ldy/16 E4M3 bytes.
+ *   y_scale       in, FP8 and NVFP4 only (else NULL): the output's static decode
+ *                 scale, as for qg_gemm_quant and qg_gemm_quant_nvfp4.
+ * Result: with y' the value of the formula from a z within qg_gemm's accuracy
+ * contract, evaluated in fp32 (relative error of the activation: SiLU and
+ * tanh-GELU at most (6 + 4 |t|) 2^-23, t the exponent's argument, z or
+ * 2 sqrt(2 / pi) (z + 0.044715 z^3); erf-GELU (20 + 2 z^2) 2^-23; below 2^-100 it may
+ * be 0), then rounded to y_dtype, or quantized by the steps of qg_gemm_quant /
+ * qg_gemm_quant_nvfp4.
+ * k = 0: z is 0. Shapes: n % 16 == 0 and the rest as for qg_gemm (gated: with
+ * 2 n weight rows).
+ */
+typedef struct qg_epilogue {
+    int32_t act;
+    int32_t gated;
+    const void *bias;
+    const void *residual;
+    int64_t ldr;
+    int32_t bias_dtype;
+    int32_t residual_dtype;
+} qg_epilogue;
+
+qg_status qg_gemm_fused(qg_format a_fmt, const void *a, const void *a_block_scales,
+                        const float *a_tensor_scale, int64_t lda,
+                        qg_format w_fmt, const void *w_packed, size_t w_packed_bytes,
+                        int64_t m, int64_t n, int64_t k, const qg_epilogue *epilogue,
+                        void *y, void *y_block_scales, int64_t ldy, qg_out_dtype y_dtype,
+                        const float *y_scale, void *stream);
+
+/*
+ * qg_rms_norm -- what stands in front of a quantized linear, in one pass: the
+ * residual's addition, the root-mean-square norm and the quantization.
+ *   h = bf16(x + residual)  (h = x without one),
+ *   y_j = fl(fl(h_j r) w_j),  r = fl(1 / fl(sqrt(fl(fl(sum_j h_j^2 / cols) + eps)))),
+ * the squares summed in fp32 (an order fixed by cols); y is the norm of the
+ * stored h. Paper: Sec. 4, quantization paragraph (activations quantized at run
+ * time for the low-precision linears).
+ *   fmt           format of y: QG_FMT_BF16, or codes quantized from the fp32 y by
+ *                 the steps of qg_quantize_act (QG_FMT_FP8_E4M3, QG_FMT_NVFP4 with
+ *                 the tensor scale taken from the largest |y|; QG_FMT_MXFP4,
+ *                 QG_FMT_MXFP8).
+ *   x             bf16 [rows, ldx].
+ *   residual      bf16 [rows, ldr] or NULL.
+ *   weight        [cols] of weight_dtype (QG_OUT_BF16 or QG_OUT_F32), aligned to an element.
+ *   eps           finite and >= 0 (a row of zeros gives zeros also at 0).
+ *   sum           out: h, bf16 [rows, lds], or NULL; NULL without a residual. It
+ *                 may be x or residual itself (same pointer and pitch).
+ *   y             out: bf16 [rows, ldy], or dense codes as qg_quantize_act's (ldy
+ *                 is then not used; NVFP4 8-byte, MXFP4 4-byte aligned).
+ *   block_scales  out: dense as qg_quantize_act's (NVFP4, MX; else NULL).
+ *   tensor_scale  out: FP8 and NVFP4 (else NULL).
+ * Except where said, no two buffers overlap. Rows of any alignment and length
+ * (any cols for bf16 and FP8; NVFP4 cols % 16 == 0, MX cols % 32 == 0, else
+ * QG_ERR_SHAPE). Squares past fp32's range are summed scaled, so finite rows
+ * give finite norms; a row holding inf or NaN gives NaN (bf16 output) or
+ * unspecified codes, and the tensor scale NaN. An empty tensor gets
+ * tensor_scale = 0.
+ */
+qg_status qg_rms_norm(qg_format fmt, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                      const void *weight, qg_out_dtype weight_dtype, float eps, int64_t rows, int64_t cols,
+                      void *sum, int64_t lds, void *y, int64_t ldy, void *block_scales,
+                      float *tensor_scale, void *stream);
+
+/*
+ * qg_rms_norm_static -- qg_rms_norm quantizing with a static (calibrated)
+ * decode scale, one launch: tensor_scale is read, as in qg_quantize_act_static
+ * (its conditions too). QG_FMT_FP8_E4M3 and QG_FMT_NVFP4 only, else
+ * QG_ERR_UNSUPPORTED. An empty tensor enqueues nothing.
+ */
+qg_status qg_rms_norm_static(qg_format fmt, const void *x, int64_t ldx, const void *residual, int64_t ldr,
+                             const void *weight, qg_out_dtype weight_dtype, float eps, int64_t rows, int64_t cols,
+                             void *sum, int64_t lds, void *y, int64_t ldy, void *block_scales,
+                             const float *tensor_scale, void *stream);
 
 /*
  * qg_dequant -- decode a quantized tensor to bf16 or fp32.

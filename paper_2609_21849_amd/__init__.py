@@ -8,7 +8,8 @@ is missing this module raises instead of computing anything elsewhere.
 
 A few helpers below (``quantize``, ``pack``, ``linear`` ...) allocate the
 output tensors with torch and then call the same entry points. The per-call
-ones (``quantize``, ``linear``, ``linear_fp8``) do so natively
+ones (``quantize``, ``linear``, ``linear_fp8``, ``linear_fused``, ``linear_gated``,
+``rms_norm``) do so natively
 (``csrc/torch_binding.cpp``) for plain CUDA tensors that pass their checks;
 anything else takes the Python statements below, which raise what is wrong, and
 so does everything where that extension was not built (with a warning: the
@@ -25,13 +26,14 @@ LIB_PATH = os.path.join(HERE, "libqgemm.so")
 
 QG_FMT_BF16, QG_FMT_FP8_E4M3, QG_FMT_NVFP4, QG_FMT_MXFP4, QG_FMT_MXFP8 = 0, 1, 2, 3, 4
 MX_FORMATS = (QG_FMT_MXFP4, QG_FMT_MXFP8)
-QG_OUT_BF16, QG_OUT_F32 = 0, 1
+QG_OUT_BF16, QG_OUT_F32, QG_OUT_FP8, QG_OUT_NVFP4 = 0, 1, 2, 3
+QG_ACT_NONE, QG_ACT_SILU, QG_ACT_GELU_TANH, QG_ACT_GELU_ERF = 0, 1, 2, 3
 QG_OK = 0
 STATUS_NAMES = {0: "QG_OK", 1: "QG_ERR_INVALID_ARG", 2: "QG_ERR_UNSUPPORTED", 3: "QG_ERR_SHAPE",
                 4: "QG_ERR_BUFFER_TOO_SMALL", 5: "QG_ERR_HIP"}
 EXPORTS = ["qg_quantize_act", "qg_quantize_act_static", "qg_packed_bytes", "qg_pack_weights", "qg_unpack_weights", "qg_gemm",
            "qg_linear_fp8",
-           "qg_gemm_quant", "qg_gemm_quant_nvfp4", "qg_dequant", "qg_run_layers", "qg_stream_simulate", "qg_stream_plan", "qg_status_string",
+           "qg_gemm_quant", "qg_gemm_quant_nvfp4", "qg_gemm_fused", "qg_rms_norm", "qg_rms_norm_static", "qg_dequant", "qg_run_layers", "qg_stream_simulate", "qg_stream_plan", "qg_status_string",
            "qg_last_hip_error", "qg_abi_version"]
 
 
@@ -42,6 +44,13 @@ class StreamLayer(ctypes.Structure):
                 ("w_fmt", ctypes.c_int), ("w_packed", ctypes.c_void_p), ("w_packed_bytes", ctypes.c_size_t),
                 ("resident", ctypes.c_int32), ("m", ctypes.c_int64), ("n", ctypes.c_int64), ("k", ctypes.c_int64),
                 ("y", ctypes.c_void_p), ("y_dtype", ctypes.c_int)]
+
+
+class Epilogue(ctypes.Structure):
+    """qg_epilogue of include/qgemm.h."""
+    _fields_ = [("act", ctypes.c_int32), ("gated", ctypes.c_int32), ("bias", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("ldr", ctypes.c_int64), ("bias_dtype", ctypes.c_int32),
+                ("residual_dtype", ctypes.c_int32)]
 
 
 class QGError(RuntimeError):
@@ -80,6 +89,12 @@ def lib() -> ctypes.CDLL:
         L.qg_gemm_quant.argtypes = [I32, P, P, P, I64, I32, P, SZ, I64, I64, I64, P, I64, P, P]
         L.qg_gemm_quant_nvfp4.restype = I32
         L.qg_gemm_quant_nvfp4.argtypes = [I32, P, P, P, I64, I32, P, SZ, I64, I64, I64, P, P, I64, P, P]
+        L.qg_gemm_fused.restype = I32
+        L.qg_gemm_fused.argtypes = [I32, P, P, P, I64, I32, P, SZ, I64, I64, I64, ctypes.POINTER(Epilogue), P, P, I64, I32,
+                                    P, P]
+        for norm in (L.qg_rms_norm, L.qg_rms_norm_static):
+            norm.restype = I32
+            norm.argtypes = [I32, P, I64, P, I64, P, I32, ctypes.c_float, I64, I64, P, I64, P, I64, P, P, P]
         L.qg_dequant.restype = I32
         L.qg_dequant.argtypes = [I32, P, P, P, I64, I64, P, I32, P]
         D, U8 = ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_uint8)
@@ -104,7 +119,7 @@ _host = None
 
 class _NoNative:
     """Stands in for the native helpers where they are not built: takes no call."""
-    quantize = linear = linear_fp8 = staticmethod(lambda *args: None)
+    quantize = linear = linear_fp8 = linear_fused = rms_norm = staticmethod(lambda *args: None)
 
 
 def _native():
@@ -117,7 +132,7 @@ def _native():
             from . import _qgemm_torch as host
         except ImportError as e:
             import warnings
-            warnings.warn("_qgemm_torch.so is not available (%s): quantize, linear and linear_fp8 run through ctypes; "
+            warnings.warn("_qgemm_torch.so is not available (%s): quantize, rms_norm and the linears run through ctypes; "
                           "`python -m paper_2609_21849_amd.build` builds it" % e, RuntimeWarning, stacklevel=3)
             host = _NoNative
         _host = host
@@ -269,6 +284,35 @@ def qg_gemm_quant_nvfp4(a_fmt, a, a_block_scales, a_tensor_scale, lda, w_fmt, w_
                                   _p(y_tensor_scale), _stream(stream))
     if check:
         _check(s, "qg_gemm_quant_nvfp4")
+    return s
+
+
+def qg_gemm_fused(a_fmt, a, a_block_scales, a_tensor_scale, lda, w_fmt, w_packed, w_packed_bytes, m, n, k, epilogue,
+                  y, y_block_scales, ldy, y_dtype, y_scale=None, stream=None, check=True):
+    """epilogue: an Epilogue (its pointers are ints), or None."""
+    s = lib().qg_gemm_fused(a_fmt, _p(a), _p(a_block_scales), _p(a_tensor_scale), lda, w_fmt, _p(w_packed),
+                            w_packed_bytes, m, n, k, None if epilogue is None else ctypes.byref(epilogue), _p(y),
+                            _p(y_block_scales), ldy, y_dtype, _p(y_scale), _stream(stream))
+    if check:
+        _check(s, "qg_gemm_fused")
+    return s
+
+
+def qg_rms_norm(fmt, x, ldx, residual, ldr, weight, weight_dtype, eps, rows, cols, sum, lds, y, ldy, block_scales,
+                tensor_scale, stream=None, check=True):
+    s = lib().qg_rms_norm(fmt, _p(x), ldx, _p(residual), ldr, _p(weight), weight_dtype, eps, rows, cols, _p(sum), lds,
+                          _p(y), ldy, _p(block_scales), _p(tensor_scale), _stream(stream))
+    if check:
+        _check(s, "qg_rms_norm")
+    return s
+
+
+def qg_rms_norm_static(fmt, x, ldx, residual, ldr, weight, weight_dtype, eps, rows, cols, sum, lds, y, ldy, block_scales,
+                       tensor_scale, stream=None, check=True):
+    s = lib().qg_rms_norm_static(fmt, _p(x), ldx, _p(residual), ldr, _p(weight), weight_dtype, eps, rows, cols, _p(sum),
+                                 lds, _p(y), ldy, _p(block_scales), _p(tensor_scale), _stream(stream))
+    if check:
+        _check(s, "qg_rms_norm_static")
     return s
 
 
@@ -504,6 +548,172 @@ def linear(a, w_packed, w_fmt: int, n: int, out_dtype: int = QG_OUT_BF16, y=None
     ldy = y.stride(0) if m > 1 else n
     qg_gemm(a_fmt, a_data, a_bs, a_ts, lda, w_fmt, w_packed, w_packed.numel(), m, n, k, y, ldy, out_dtype, stream)
     return y
+
+
+def _current_device(dev) -> None:
+    import torch
+    if dev.index != torch.cuda.current_device():
+        raise ValueError("tensors on %s, but the current device is cuda:%d" % (dev, torch.cuda.current_device()))
+
+
+def _dtype_code(t, name: str) -> int:
+    import torch
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise ValueError("%s: expected dtype torch.bfloat16 or torch.float32, got %s" % (name, t.dtype))
+    return QG_OUT_F32 if t.dtype == torch.float32 else QG_OUT_BF16
+
+
+def _pitch(t) -> int:
+    """Elements between the rows of a 2-D tensor (a size-1 dimension may carry any stride)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _linear_epilogue(a, w_packed, w_fmt, n, bias, act, residual, gated, out_dtype, y_scale, y, stream):
+    native = (_host or _native()).linear_fused
+    if type(a) is QTensor:
+        r = native(a.fmt, a.codes, a.block_scales, a.tensor_scale, a.rows, a.cols, w_packed, w_fmt, n, out_dtype, y,
+                   _handle(stream), bias, act, residual, gated, y_scale)
+    else:
+        r = native(QG_FMT_BF16, a, None, None, 0, 0, w_packed, w_fmt, n, out_dtype, y, _handle(stream), bias, act, residual,
+                   gated, y_scale)
+    if r is not None:
+        if type(r) is int:
+            _check(r, "qg_gemm_fused")
+        if out_dtype in (QG_OUT_BF16, QG_OUT_F32):
+            return r
+        return QTensor(QG_FMT_FP8_E4M3 if out_dtype == QG_OUT_FP8 else QG_FMT_NVFP4, r[0], r[1], y_scale, r[0].shape[0], n)
+    import torch
+    m, k, a_fmt, a_data, a_bs, a_ts, lda, dev = _operands(a, w_packed)
+    _current_device(dev)
+    if out_dtype not in (QG_OUT_BF16, QG_OUT_F32, QG_OUT_FP8, QG_OUT_NVFP4):
+        raise ValueError("out_dtype must be QG_OUT_BF16, QG_OUT_F32, QG_OUT_FP8 or QG_OUT_NVFP4")
+    e = Epilogue(act=act, gated=1 if gated else 0)
+    if bias is not None:
+        e.bias_dtype = _dtype_code(bias, "bias")
+        _need(bias, "bias", bias.dtype, (2 * n if gated else n,), dev)
+        e.bias = bias.data_ptr()
+    if residual is not None:
+        e.residual_dtype = _dtype_code(residual, "residual")
+        _need(residual, "residual", residual.dtype, (m, n), dev, dense=False)
+        e.residual, e.ldr = residual.data_ptr(), _pitch(residual)
+    bs = None
+    if out_dtype in (QG_OUT_FP8, QG_OUT_NVFP4):
+        if y is not None:
+            raise ValueError("y: quantized outputs are allocated by the call")
+        if y_scale is None:
+            raise ValueError("y_scale: a quantized output needs its decode scale")
+        _need(y_scale, "y_scale", torch.float32, None, dev)
+        if y_scale.numel() < 1:
+            raise ValueError("y_scale: expected one element")
+        y = torch.empty((m, n if out_dtype == QG_OUT_FP8 else n // 2), dtype=torch.uint8, device=dev)
+        if out_dtype == QG_OUT_NVFP4:
+            bs = torch.empty((m, n // 16), dtype=torch.uint8, device=dev)
+        ldy = n
+    else:
+        if y_scale is not None:
+            raise ValueError("y_scale: only for QG_OUT_FP8 and QG_OUT_NVFP4")
+        ydt = torch.float32 if out_dtype == QG_OUT_F32 else torch.bfloat16
+        if y is None:
+            y = torch.empty((m, n), dtype=ydt, device=dev)
+        else:
+            _need(y, "y", ydt, (m, n), dev, dense=False)
+        ldy = _pitch(y)
+    qg_gemm_fused(a_fmt, a_data, a_bs, a_ts, lda, w_fmt, w_packed, w_packed.numel(), m, n, k, e, y, bs, ldy, out_dtype,
+                  y_scale, stream)
+    if out_dtype in (QG_OUT_BF16, QG_OUT_F32):
+        return y
+    return QTensor(QG_FMT_FP8_E4M3 if out_dtype == QG_OUT_FP8 else QG_FMT_NVFP4, y, bs, y_scale, m, n)
+
+
+def linear_fused(a, w_packed, w_fmt: int, n: int, bias=None, act: int = QG_ACT_NONE, residual=None,
+                 out_dtype: int = QG_OUT_BF16, y_scale=None, y=None, stream=None):
+    """Y = act(A . W^T + bias) + residual in one launch, for a quantized A
+    (QTensor) or a bf16 A against an NVFP4 weight.
+
+    bias [n] and residual [m, n] (rows of unit stride) are bf16 or fp32. Y is
+    bf16 or fp32, or with QG_OUT_FP8 / QG_OUT_NVFP4 and a static decode scale
+    y_scale (a one-element fp32 CUDA tensor) a QTensor, the next linear's
+    activation. y (bf16 and fp32) receives the result; it may be residual
+    itself, no other overlap. Forward only, as every function here."""
+    return _linear_epilogue(a, w_packed, w_fmt, n, bias, act, residual, False, out_dtype, y_scale, y, stream)
+
+
+def linear_gated(a, w_packed, w_fmt: int, n: int, act: int = QG_ACT_SILU, bias=None, out_dtype: int = QG_OUT_BF16,
+                 y_scale=None, y=None, stream=None):
+    """Y = act(A . Wg^T + bg) * (A . Wu^T + bu) [m, n] in one launch: the gated
+    projections of a feed-forward block. w_packed holds both weights
+    (pack_gated), bias both biases in the same order (interleave_gated).
+    Types of a, bias and Y as in linear_fused."""
+    return _linear_epilogue(a, w_packed, w_fmt, n, bias, act, None, True, out_dtype, y_scale, y, stream)
+
+
+def interleave_gated(gate, up):
+    """Rows (elements of a vector) of two equal tensors taken in turn: 2 i the
+    gate's row i, 2 i + 1 the up projection's."""
+    import torch
+    if gate.shape != up.shape or gate.dtype != up.dtype or gate.device != up.device:
+        raise ValueError("gate and up: expected the same shape, dtype and device")
+    return torch.stack((gate, up), 1).flatten(0, 1)
+
+
+def pack_gated(w_gate, w_up, fmt: int, stream=None):
+    """Quantize and pack the two bf16 weights [n, k] of linear_gated, as one
+    tensor (FP8 and NVFP4: with one tensor scale)."""
+    return pack(quantize(interleave_gated(w_gate, w_up), fmt, stream), stream)
+
+
+def rms_norm(x, weight, eps: float = 1e-6, residual=None, fmt: int = QG_FMT_BF16, static_scale=None, sum_out=None,
+             stream=None):
+    """Root-mean-square norm of bf16 rows x [rows, cols], or with a residual of
+    their rounded sum h = x + residual, in the format `fmt`: a bf16 tensor, or
+    a QTensor that a linear takes as it is (static_scale: a calibrated FP8 or
+    NVFP4 decode scale, a one-element fp32 CUDA tensor).
+
+    Returns y, with a residual (y, h). h goes to sum_out if given, which may be
+    x or residual. weight [cols] is bf16 or fp32. Forward only."""
+    r = (_host or _native()).rms_norm(x, weight, eps, residual, fmt, static_scale, sum_out, _handle(stream))
+    if r is not None:
+        if type(r) is int:
+            _check(r, "qg_rms_norm" if static_scale is None else "qg_rms_norm_static")
+        y, bs, ts, h, rows, cols = r
+        y = y if fmt == QG_FMT_BF16 else QTensor(fmt, y, bs, ts, rows, cols)
+        return y if residual is None else (y, h)
+    import torch
+    _need(x, "x", torch.bfloat16, dense=False)
+    rows, cols = x.shape
+    dev = x.device
+    _current_device(dev)
+    wdt = _dtype_code(weight, "weight")
+    _need(weight, "weight", weight.dtype, (cols,), dev)
+    h = None
+    if residual is not None:
+        _need(residual, "residual", torch.bfloat16, (rows, cols), dev, dense=False)
+        h = torch.empty((rows, cols), dtype=torch.bfloat16, device=dev) if sum_out is None else sum_out
+        _need(h, "sum_out", torch.bfloat16, (rows, cols), dev, dense=False)
+    elif sum_out is not None:
+        raise ValueError("sum_out: there is no sum without a residual")
+    bs = None
+    if fmt == QG_FMT_BF16:
+        y = torch.empty((rows, cols), dtype=torch.bfloat16, device=dev)
+    elif fmt in (QG_FMT_FP8_E4M3, QG_FMT_MXFP8):
+        y = torch.empty((rows, cols), dtype=torch.uint8, device=dev)
+    else:
+        y = torch.empty((rows, cols // 2), dtype=torch.uint8, device=dev)
+    if fmt in (QG_FMT_NVFP4, *MX_FORMATS):
+        bs = torch.empty((rows, cols // (16 if fmt == QG_FMT_NVFP4 else 32)), dtype=torch.uint8, device=dev)
+    ts = None
+    if static_scale is not None:
+        _need(static_scale, "static_scale", torch.float32, None, dev)
+        if static_scale.numel() < 1:
+            raise ValueError("static_scale: expected one element")
+        ts = static_scale
+    elif fmt in (QG_FMT_FP8_E4M3, QG_FMT_NVFP4):
+        ts = torch.empty(1, dtype=torch.float32, device=dev)
+    run = qg_rms_norm if static_scale is None else qg_rms_norm_static
+    run(fmt, x, _pitch(x), residual, 0 if residual is None else _pitch(residual), weight, wdt, eps, rows, cols, h,
+        0 if h is None else _pitch(h), y, cols, bs, ts, stream)
+    y = y if fmt == QG_FMT_BF16 else QTensor(fmt, y, bs, ts, rows, cols)
+    return y if residual is None else (y, h)
 
 
 def dequantize(q: QTensor, out_dtype: int = QG_OUT_F32, stream=None):

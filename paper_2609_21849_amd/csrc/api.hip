@@ -6,6 +6,7 @@
 // these checks can be exercised on a machine without a GPU.
 #include <hip/hip_runtime.h>
 
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <limits>
@@ -351,6 +352,120 @@ qg_status qg_gemm_quant_nvfp4(qg_format a_fmt, const void* a, const void* a_bloc
     qg::log_call("qg_gemm_quant_nvfp4", st_, "a_fmt=%d w_fmt=%d m=%lld n=%lld k=%lld lda=%lld ldy=%lld",
                  (int)a_fmt, (int)w_fmt, (long long)m, (long long)n, (long long)k, (long long)lda,
                  (long long)ldy);
+  return st_;
+}
+
+qg_status qg_gemm_fused(qg_format a_fmt, const void* a, const void* a_block_scales, const float* a_tensor_scale,
+                        int64_t lda, qg_format w_fmt, const void* w_packed, size_t w_packed_bytes, int64_t m, int64_t n,
+                        int64_t k, const qg_epilogue* ep, void* y, void* y_block_scales, int64_t ldy,
+                        qg_out_dtype y_dtype, const float* y_scale, void* stream) {
+  const qg_status st_ = [&]() -> qg_status {
+    if (ep == nullptr || (ep->gated != 0 && ep->gated != 1) || ep->act < QG_ACT_NONE || ep->act > QG_ACT_GELU_ERF)
+      return QG_ERR_INVALID_ARG;
+    if (y_dtype < QG_OUT_BF16 || y_dtype > QG_OUT_NVFP4) return QG_ERR_INVALID_ARG;
+    const bool nv = y_dtype == QG_OUT_NVFP4, scaled = nv || y_dtype == QG_OUT_FP8;
+    if (scaled ? (y_scale == nullptr || !aligned(y_scale, 4)) : y_scale != nullptr) return QG_ERR_INVALID_ARG;
+    if (m < 0 || n < 0 || k < 0 || n > kMaxDim) return QG_ERR_INVALID_ARG;
+    if (n % 16 != 0) return QG_ERR_SHAPE;
+    // the product's own checks, over the weight's rows; y's pitch is checked below
+    const int64_t rows = ep->gated ? 2 * n : n;
+    const qg_status c = qg::check_gemm(a_fmt, a, a_block_scales, a_tensor_scale, lda, w_fmt, w_packed, w_packed_bytes,
+                                       m, rows, k, y, rows, nv || y_dtype == QG_OUT_F32 ? 4 : y_dtype == QG_OUT_FP8 ? 1 : 2);
+    if (c != QG_OK) return c;
+    if (nv && a_fmt == QG_FMT_BF16) return QG_ERR_UNSUPPORTED;
+    if (m > 0 && (ldy < n || (nv && ldy % 16 != 0))) return QG_ERR_INVALID_ARG;
+    if (nv ? (m > 0 && n > 0 && y_block_scales == nullptr) : y_block_scales != nullptr) return QG_ERR_INVALID_ARG;
+    if (nv && m > 0 && ((m - 1) * ldy + n) / 2 > kMaxDim) return QG_ERR_SHAPE;
+    const auto dtype_ok = [](int d) { return d == QG_OUT_BF16 || d == QG_OUT_F32; };
+    const auto esz = [](int d) -> uintptr_t { return d == QG_OUT_F32 ? 4 : 2; };
+    if (ep->bias && (!dtype_ok(ep->bias_dtype) || !aligned(ep->bias, esz(ep->bias_dtype)))) return QG_ERR_INVALID_ARG;
+    if (ep->residual && (ep->gated || !dtype_ok(ep->residual_dtype) || !aligned(ep->residual, esz(ep->residual_dtype)) ||
+                         (m > 0 && ep->ldr < n)))
+      return QG_ERR_INVALID_ARG;
+    qg::Epilogue e = {};
+    e.bias = ep->bias;
+    e.bias_f32 = ep->bias_dtype == QG_OUT_F32;
+    e.residual = ep->residual;
+    e.res_f32 = ep->residual_dtype == QG_OUT_F32;
+    e.ldr = ep->residual ? ep->ldr : 0;
+    e.act = ep->act;
+    const auto launch = ep->gated ? qg::gated::launch : qg::fused::launch;
+    return hip_status(launch((int)a_fmt, a, reinterpret_cast<const uint8_t*>(a_block_scales), a_tensor_scale, lda,
+                             reinterpret_cast<const uint8_t*>(w_packed), m, rows, k, e, y, ldy, (int)y_dtype, y_scale,
+                             reinterpret_cast<uint8_t*>(y_block_scales), reinterpret_cast<hipStream_t>(stream)));
+  }();
+  if (qg::log_enabled())
+    qg::log_call("qg_gemm_fused", st_,
+                 "a_fmt=%d w_fmt=%d m=%lld n=%lld k=%lld lda=%lld ldy=%lld y_dtype=%d act=%d gated=%d bias=%d residual=%d",
+                 (int)a_fmt, (int)w_fmt, (long long)m, (long long)n, (long long)k, (long long)lda, (long long)ldy,
+                 (int)y_dtype, ep ? (int)ep->act : -1, ep ? (int)ep->gated : -1, ep && ep->bias ? 1 : 0,
+                 ep && ep->residual ? 1 : 0);
+  return st_;
+}
+
+static qg_status rms_norm(qg_format fmt, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                          const void* weight, qg_out_dtype weight_dtype, float eps, int64_t rows, int64_t cols,
+                          void* sum, int64_t lds, void* y, int64_t ldy, void* block_scales, const float* tensor_scale,
+                          bool static_scale, void* stream) {
+  if (!valid_fmt(fmt)) return QG_ERR_INVALID_ARG;
+  const bool scaled = fmt == QG_FMT_FP8_E4M3 || fmt == QG_FMT_NVFP4;
+  if (static_scale && !scaled) return QG_ERR_UNSUPPORTED;
+  if (weight_dtype != QG_OUT_BF16 && weight_dtype != QG_OUT_F32) return QG_ERR_INVALID_ARG;
+  if (!std::isfinite(eps) || eps < 0.0f) return QG_ERR_INVALID_ARG;
+  if (rows < 0 || cols < 0 || rows > kMaxDim || cols > kMaxDim) return QG_ERR_INVALID_ARG;
+  if (scaled ? (tensor_scale == nullptr || !aligned(tensor_scale, 4)) : tensor_scale != nullptr) return QG_ERR_INVALID_ARG;
+  if (fmt == QG_FMT_NVFP4 && cols % 16 != 0) return QG_ERR_SHAPE;
+  if (is_mx(fmt) && cols % 32 != 0) return QG_ERR_SHAPE;
+  const bool blocks = fmt == QG_FMT_NVFP4 || is_mx(fmt);
+  if (!blocks && block_scales != nullptr) return QG_ERR_INVALID_ARG;
+  if (sum != nullptr && residual == nullptr) return QG_ERR_INVALID_ARG;
+  if (rows > 0 && cols > 0) {
+    if (ldx < cols || (residual && ldr < cols) || (sum && lds < cols) || (fmt == QG_FMT_BF16 && ldy < cols))
+      return QG_ERR_INVALID_ARG;
+    if (x == nullptr || !aligned(x, 2) || !aligned(residual, 2) || !aligned(sum, 2)) return QG_ERR_INVALID_ARG;
+    if (weight == nullptr || !aligned(weight, weight_dtype == QG_OUT_F32 ? 4 : 2)) return QG_ERR_INVALID_ARG;
+    const uintptr_t y_align = fmt == QG_FMT_BF16 ? 2 : fmt == QG_FMT_NVFP4 ? 8 : fmt == QG_FMT_MXFP4 ? 4 : 1;
+    if (y == nullptr || !aligned(y, y_align) || (blocks && block_scales == nullptr)) return QG_ERR_INVALID_ARG;
+  }
+  qg::NormArgs a = {};
+  a.x = reinterpret_cast<const uint16_t*>(x);
+  a.ldx = ldx;
+  a.res = reinterpret_cast<const uint16_t*>(residual);
+  a.ldr = ldr;
+  a.w = weight;
+  a.w_f32 = weight_dtype == QG_OUT_F32;
+  a.eps = eps;
+  a.rows = rows;
+  a.cols = (int)cols;
+  a.sum = reinterpret_cast<uint16_t*>(sum);
+  a.lds = lds;
+  a.y = reinterpret_cast<uint8_t*>(y);
+  a.ldy = ldy;
+  a.bscale = reinterpret_cast<uint8_t*>(block_scales);
+  a.tscale = const_cast<float*>(tensor_scale);
+  return hip_status(qg::launch_rms_norm((int)fmt, a, static_scale, reinterpret_cast<hipStream_t>(stream)));
+}
+
+qg_status qg_rms_norm(qg_format fmt, const void* x, int64_t ldx, const void* residual, int64_t ldr, const void* weight,
+                      qg_out_dtype weight_dtype, float eps, int64_t rows, int64_t cols, void* sum, int64_t lds, void* y,
+                      int64_t ldy, void* block_scales, float* tensor_scale, void* stream) {
+  const qg_status st_ = rms_norm(fmt, x, ldx, residual, ldr, weight, weight_dtype, eps, rows, cols, sum, lds, y, ldy,
+                                 block_scales, tensor_scale, false, stream);
+  if (qg::log_enabled())
+    qg::log_call("qg_rms_norm", st_, "fmt=%d rows=%lld cols=%lld ldx=%lld residual=%d sum=%d", (int)fmt, (long long)rows,
+                 (long long)cols, (long long)ldx, residual ? 1 : 0, sum ? 1 : 0);
+  return st_;
+}
+
+qg_status qg_rms_norm_static(qg_format fmt, const void* x, int64_t ldx, const void* residual, int64_t ldr,
+                             const void* weight, qg_out_dtype weight_dtype, float eps, int64_t rows, int64_t cols,
+                             void* sum, int64_t lds, void* y, int64_t ldy, void* block_scales, const float* tensor_scale,
+                             void* stream) {
+  const qg_status st_ = rms_norm(fmt, x, ldx, residual, ldr, weight, weight_dtype, eps, rows, cols, sum, lds, y, ldy,
+                                 block_scales, tensor_scale, true, stream);
+  if (qg::log_enabled())
+    qg::log_call("qg_rms_norm_static", st_, "fmt=%d rows=%lld cols=%lld ldx=%lld residual=%d sum=%d", (int)fmt,
+                 (long long)rows, (long long)cols, (long long)ldx, residual ? 1 : 0, sum ? 1 : 0);
   return st_;
 }
 

@@ -176,4 +176,36 @@ __device__ inline uint32_t hw_e4m3x4(const float* y) {
   return __builtin_bit_cast(uint32_t, w);
 }
 
+// ---------------------------------------------------------------------------
+// Block scales of quantized fp32 values (GEMM epilogues, the norm, MX quantizer).
+// E4M3 block scale of a block whose largest |y| has the bit pattern amax,
+// and the reciprocal r its elements are multiplied by.
+__device__ __attribute__((always_inline)) inline uint32_t nv_block(uint32_t amax, float st, float d, float& r) {
+  const float vb = (d > 0.0f) ? __fdiv_rn(u2f(amax), d) : 0.0f;
+  const uint32_t sb = enc_e4m3(vb);
+  const float S = __fmul_rn(dec_e4m3(sb), st);
+  r = (S > 0.0f) ? __fdiv_rn(1.0f, S) : 0.0f;
+  return sb;
+}
+
+// E8M0 code of a block from the fp32 bits of its largest magnitude and the
+// factor its elements are multiplied by.
+template <bool FP4>
+__device__ inline uint32_t mx_block(uint32_t am, float& r) {
+  // floor(log2(max)) from the fp32 bits (normal or denormal), then the code.
+  // A block holding inf or NaN gets the E8M0 NaN code 255 (its element codes
+  // are then unspecified: r = 0 makes them signed zeros).
+  int e = 0;
+  if (am >= 0x7F800000u) {
+    e = 255;
+  } else if (am != 0u) {
+    const int ef = (int)(am >> 23);
+    const int fl = (ef > 0) ? ef - 127 : (31 - __builtin_clz(am)) - 149;
+    e = min(max(fl - (FP4 ? 2 : 8) + 127, 0), 254);
+  }
+  // 2^(127 - e); finite bf16 inputs give e <= 252, so this is a normal number
+  r = (e == 255) ? 0.0f : u2f((uint32_t)(254 - e) << 23);
+  return (uint32_t)e;
+}
+
 }  // namespace qg

@@ -39,14 +39,34 @@
 // MFMA orientation: the weight panel is the MFMA A operand and the
 // activation panel the B operand, so a lane ends with runs of 4 consecutive
 // output columns of one output row.
+//
+// What the kernels do with the finished sums is a choice of the translation unit
+// (QG_EPILOGUE), since behind run-time branches in one kernel the main loop loses
+// registers: 0, this file by itself, rounds and stores them (qg_gemm and its
+// quantized outputs); gemm_fused.hip (1) adds bias, activation and residual and
+// gemm_gated.hip (2) multiplies the activated gate with its up projection before
+// that (qg_gemm_fused), with the same kernels in namespaces of their own.
 #include <algorithm>
 #include <type_traits>
+#include <utility>
 
 #include "common.hpp"
 #include "kernels.hpp"
+#include "qgemm.h"
 #include "tile_plan.hpp"
 
+#ifndef QG_EPILOGUE
+#define QG_EPILOGUE 0
+#endif
+
 namespace qg {
+#if QG_EPILOGUE == 1
+namespace fused {
+#elif QG_EPILOGUE == 2
+namespace gated {
+#endif
+
+constexpr bool kFused = QG_EPILOGUE == 1, kGated = QG_EPILOGUE == 2;
 
 enum { MODE_W4A16 = 0, MODE_FP8 = 1, MODE_NVFP4 = 2, MODE_MXFP4 = 3, MODE_MXFP8 = 4 };  // format ids
 
@@ -67,6 +87,9 @@ struct GemmArgs {
   const float* y_scale;     // decode scale of the FP8 output / tensor scale of the NVFP4 output
   uint8_t* y_bscale;        // NVFP4 output: E4M3 block scales [m, ldy / 16]
   int tiles_m, tiles_n;
+#if QG_EPILOGUE
+  Epilogue e;
+#endif
 };
 
 constexpr int OUT_BF16 = 0, OUT_F32 = 1, OUT_FP8 = 2, OUT_NVFP4 = 3;
@@ -123,16 +146,6 @@ __device__ __attribute__((always_inline)) inline float nv_out_d(const GemmArgs& 
   return g.out_mode == OUT_NVFP4 ? __fmul_rn(6.0f, *g.y_scale) : 0.0f;
 }
 
-// E4M3 block scale of a block whose largest |y| has the bit pattern amax,
-// and the reciprocal r its elements are multiplied by.
-__device__ __attribute__((always_inline)) inline uint32_t nv_block(uint32_t amax, float st, float d, float& r) {
-  const float vb = (d > 0.0f) ? __fdiv_rn(u2f(amax), d) : 0.0f;
-  const uint32_t sb = enc_e4m3(vb);
-  const float S = __fmul_rn(dec_e4m3(sb), st);
-  r = (S > 0.0f) ? __fdiv_rn(1.0f, S) : 0.0f;
-  return sb;
-}
-
 // One 16-block of a row held by a lane pair in the MFMA output layout: lane
 // half g holds columns 4 g + [0, 4) of the block in v[0..3] and 8 + 4 g +
 // [0, 4) in v[4..7]. Both lanes of the pair (l, l ^ 32) call this together;
@@ -186,6 +199,281 @@ __device__ __attribute__((always_inline)) inline void store_nv_quad(const GemmAr
   *reinterpret_cast<uint16_t*>(row + (n >> 1)) = (uint16_t)w;
   if ((n & 15) == 0) g.y_bscale[(int64_t)m * (g.ldy >> 4) + (n >> 4)] = (uint8_t)sb;
 }
+
+#if QG_EPILOGUE
+// ---------------------------------------------------------------- bias, activation, residual, gate
+// y = act(z + bias) + residual (kFused) or act(z_gate + bias) (z_up + bias)
+// (kGated: weight rows, and so accumulator columns, 2 i and 2 i + 1 are output
+// i's gate and up rows), z the sum times the tensor scales: every step in fp32, one
+// rounding at the store. The exponential is the hardware's 2^x of z log2 e: its
+// argument's rounding leaves a relative error of |z| 2^-24, below the bf16 and FP8
+// outputs' half steps for any |z| with a nonzero result.
+//   SiLU       z / (1 + e^-z)
+//   GELU tanh  z / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3): 0.5 (1 + tanh u) is
+//              the logistic function of 2 u
+//   GELU erf   z erfc(-z / sqrt 2) / 2, without the cancellation of 1 + erf at z < 0
+// Far negative z: the exponential is inf, its reciprocal 0, the result -0.
+__device__ __attribute__((always_inline)) inline float logistic(float t) {
+  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504f));
+}
+
+template <int W>
+__device__ __attribute__((always_inline)) inline void activate(float (&v)[W], int act) {
+  if (act == QG_ACT_SILU) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] *= logistic(v[i]);
+  } else if (act == QG_ACT_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] *= logistic(1.59576912f * v[i] * (1.0f + 0.044715f * v[i] * v[i]));
+  } else if (act == QG_ACT_GELU_ERF) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] *= 0.5f * erfcf(-0.70710678f * v[i]);
+  }
+}
+
+// W (4 or 8) consecutive elements of a bf16 or fp32 row from element `at` of p on (a
+// multiple of W), as they lie in memory; vec: such runs allow wide loads.
+template <int W>
+struct Run {
+  uint32_t w[W];  // bf16: W / 2 pairs; fp32: W values
+};
+template <int W>
+__device__ __attribute__((always_inline)) inline Run<W> load_run(const void* p, int64_t at, bool f32, bool vec) {
+  Run<W> t;
+#pragma unroll
+  for (int i = 0; i < W; ++i) t.w[i] = 0u;
+  if (f32) {
+    const uint32_t* q = reinterpret_cast<const uint32_t*>(p) + at;
+    if (vec) {
+#pragma unroll
+      for (int i = 0; i < W; i += 4) {
+        const uint4 v = *reinterpret_cast<const uint4*>(q + i);
+        t.w[i] = v.x; t.w[i + 1] = v.y; t.w[i + 2] = v.z; t.w[i + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < W; ++i) t.w[i] = q[i];
+    }
+  } else {
+    const uint16_t* q = reinterpret_cast<const uint16_t*>(p) + at;
+    if (vec && W == 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(q);
+      t.w[0] = v.x; t.w[1] = v.y; t.w[2] = v.z; t.w[3] = v.w;
+    } else if (vec) {
+      const uint2 v = *reinterpret_cast<const uint2*>(q);
+      t.w[0] = v.x; t.w[1] = v.y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) t.w[i] = q[2 * i] | ((uint32_t)q[2 * i + 1] << 16);
+    }
+  }
+  return t;
+}
+template <int W>
+__device__ __attribute__((always_inline)) inline void add_run(float* v, const Run<W>& t, bool f32) {
+  if (f32) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) v[i] += u2f(t.w[i]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) {
+      v[2 * i] += bf16_lo(t.w[i]);
+      v[2 * i + 1] += bf16_hi(t.w[i]);
+    }
+  }
+}
+
+// Weight rows, so accumulator columns, of one output.
+constexpr int kPer = kGated ? 2 : 1;
+
+// The bias of kPer W weight rows and the residual of W outputs.
+template <int W>
+struct BiasRun {
+  Run<W> t[kPer];
+};
+template <int W>
+__device__ __attribute__((always_inline)) inline BiasRun<W> load_bias(const GemmArgs& g, int n) {
+  BiasRun<W> b;
+#pragma unroll
+  for (int h = 0; h < kPer; ++h) b.t[h] = load_run<W>(g.e.bias, n + h * W, g.e.bias_f32, g.e.bias_vec);
+  return b;
+}
+template <int W>
+__device__ __attribute__((always_inline)) inline Run<W> load_residual(const GemmArgs& g, int m, int n) {
+  return load_run<W>(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32, g.e.res_vec);
+}
+
+// W outputs from the scaled sums z of kPer W consecutive weight rows, with their
+// bias and residual (read only where g.e has them).
+template <int W>
+__device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, const BiasRun<W>& b, const Run<W>& res,
+                                                             float (&z)[kPer * W], float (&y)[W]) {
+  if (g.e.bias) {
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) add_run<W>(z + h * W, b.t[h], g.e.bias_f32);
+  }
+#pragma unroll
+  for (int i = 0; i < W; ++i) y[i] = z[kPer * i];
+  activate(y, g.e.act);
+  if (kGated) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) y[i] *= z[kPer * i + kPer - 1];
+  } else if (g.e.residual) {
+    add_run<W>(y, res, g.e.res_f32);
+  }
+}
+
+// The same, loading both: outputs m, n / kPer on for weight rows from n on.
+template <int W>
+__device__ __attribute__((always_inline)) inline void finish_at(const GemmArgs& g, int m, int n, float (&z)[kPer * W],
+                                                                float (&y)[W]) {
+  BiasRun<W> b = {};
+  Run<W> res = {};
+  if (g.e.bias) b = load_bias<W>(g, n);
+  if (!kGated && g.e.residual) res = load_residual<W>(g, m, n);
+  finish<W>(g, b, res, z, y);
+}
+
+// One output from the scaled sum of one column held by each lane (the weight-pool
+// kernels); false where the lane holds an up projection, whose gate's lane (one
+// lower) has the output.
+__device__ __attribute__((always_inline)) inline bool finish1(const GemmArgs& g, int m, int& n, float& z) {
+  auto at = [](const void* p, int64_t i, bool f32) {
+    return f32 ? reinterpret_cast<const float*>(p)[i] : u2f((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
+  };
+  if (g.e.bias) z += at(g.e.bias, n, g.e.bias_f32);
+  const float up = kGated ? __shfl_xor(z, 1) : 0.0f;
+  float y[1] = {z};
+  activate(y, g.e.act);
+  if (kGated) {
+    z = y[0] * up;
+    const bool gate = (n & 1) == 0;
+    n >>= 1;
+    return gate;
+  }
+  z = y[0];
+  if (g.e.residual) z += at(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32);
+  return true;
+}
+
+// Eight consecutive outputs y[m][n .. n+7] (n % 8 == 0) in the output format, by
+// the steps of store4 and store_nv_quad. NVFP4: lanes 2 j and 2 j + 1 hold the halves of
+// a 16-block and call this together.
+template <int OUT>
+__device__ __attribute__((always_inline)) inline void store8(const GemmArgs& g, int m, int n, const float (&y)[8], bool vec,
+                                                             float r, float st, float d) {
+  if constexpr (OUT == OUT_NVFP4) {
+    uint32_t am = 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) am = max(am, f2u(y[j]) & 0x7FFFFFFFu);
+    am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+    float rb;
+    const uint32_t sb = nv_block(am, st, d, rb);
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = __fmul_rn(y[j], rb);
+    uint8_t* row = reinterpret_cast<uint8_t*>(g.y) + (int64_t)m * (g.ldy >> 1);
+    *reinterpret_cast<uint32_t*>(row + (n >> 1)) = hw_e2m1x8(t);
+    if ((n & 15) == 0) g.y_bscale[(int64_t)m * (g.ldy >> 4) + (n >> 4)] = (uint8_t)sb;
+  } else if (!vec) {
+    store4(g, m, n, y[0], y[1], y[2], y[3], false, r);
+    store4(g, m, n + 4, y[4], y[5], y[6], y[7], false, r);
+  } else if constexpr (OUT == OUT_F32) {
+    float* o = reinterpret_cast<float*>(g.y) + (int64_t)m * g.ldy + n;
+    reinterpret_cast<float4*>(o)[0] = make_float4(y[0], y[1], y[2], y[3]);
+    reinterpret_cast<float4*>(o)[1] = make_float4(y[4], y[5], y[6], y[7]);
+  } else if constexpr (OUT == OUT_FP8) {
+    float t[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[j] = __fmul_rn(y[j], r);
+    *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(g.y) + (int64_t)m * g.ldy + n) =
+        make_uint2(hw_e4m3x4(t), hw_e4m3x4(t + 4));
+  } else {
+    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.y) + (int64_t)m * g.ldy + n) =
+        make_uint4(pk_bf16(y[0], y[1]), pk_bf16(y[2], y[3]), pk_bf16(y[4], y[5]), pk_bf16(y[6], y[7]));
+  }
+}
+
+// Whether store8 may use aligned stores for every row of this output.
+__device__ __attribute__((always_inline)) inline bool out_vec8(const GemmArgs& g) {
+  const int bytes = g.out_mode == OUT_FP8 ? 8 : 16, esz = g.out_mode == OUT_F32 ? 4 : g.out_mode == OUT_FP8 ? 1 : 2;
+  return ((reinterpret_cast<uintptr_t>(g.y) & (bytes - 1)) == 0) && ((g.ldy * esz & (bytes - 1)) == 0);
+}
+
+// put(b) for the one of the constants K that b is. The empty statements differ in K: the
+// compiler otherwise merges the ends of the branches, indexing accumulators that
+// it then keeps in scratch for it (288 x 192 tiles: 144 bytes).
+template <class Put, int... K>
+__device__ __attribute__((always_inline)) inline void put_block(int b, Put put, std::integer_sequence<int, K...>) {
+  auto one = [&]<int k>(std::integral_constant<int, k>) __attribute__((always_inline)) {
+    if (b == k) {
+      put(k);
+      asm volatile("" ::"n"(k));
+    }
+  };
+  (one(std::integral_constant<int, K>()), ...);
+}
+
+// The staged epilogue of a wave's sums, NB blocks of RB rows x CB columns, block b at
+// row m and column n of at(b, m, n): put(b) leaves a block in the wave's private LDS
+// area (row-major fp32, PITCH bytes a row) and every lane takes the columns of
+// eight outputs of a row, so that bias, residual and output are read and written in
+// whole row segments. Each wave reads back only what it wrote, so no barrier is needed.
+// The blocks are walked by a loop (only put is unrolled: accumulators have fixed
+// registers), the next block's residual under way while one is finished. In place
+// (residual the output) is fine: an element is read by the lane that writes it.
+template <int OUT, int NB, int RB, int CB, int PITCH, class Put, class At>
+__device__ __attribute__((always_inline)) inline void finish_blocks(const GemmArgs& g, const uint8_t* stage, int lane, float c,
+                                                                    Put put, At at) {
+  constexpr int Z = 8 * kPer, LPR = CB / Z, PIECES = RB * LPR, ITS = (PIECES + 63) / 64;
+  const bool vec = out_vec8(g);
+  const float r = OUT == OUT_FP8 ? out_rscale(g) : 0.0f;
+  const float st = OUT == OUT_NVFP4 ? *g.y_scale : 0.0f, d = nv_out_d(g);
+  int row[ITS], col[ITS];
+#pragma unroll
+  for (int it = 0; it < ITS; ++it) {
+    const int idx = it * 64 + lane;
+    row[it] = (PIECES % 64 == 0 || idx < PIECES) ? idx / LPR : 1 << 30;  // (past every output)
+    col[it] = Z * (idx % LPR);
+  }
+  Run<8> next[ITS] = {}, res[ITS] = {};
+  auto load = [&](int b) __attribute__((always_inline)) {
+    int m, n;
+    at(b, m, n);
+#pragma unroll
+    for (int it = 0; it < ITS; ++it)
+      if (row[it] < g.m - m && n + col[it] < g.n) next[it] = load_residual<8>(g, m + row[it], n + col[it]);
+  };
+  const bool residual = !kGated && g.e.residual != nullptr;
+  if (residual) load(0);
+#pragma unroll 1
+  for (int b = 0; b < NB; ++b) {
+    if (residual) {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it) res[it] = next[it];
+      if (b + 1 < NB) load(b + 1);
+    }
+    put_block(b, put, std::make_integer_sequence<int, NB>());
+    int m, n;
+    at(b, m, n);
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const int mm = m + row[it], nn = n + col[it];
+      if (row[it] >= g.m - m || nn >= g.n) continue;
+      BiasRun<8> bias = {};
+      if (g.e.bias) bias = load_bias<8>(g, nn);
+      float z[Z], y[8];
+#pragma unroll
+      for (int i = 0; i < Z; i += 4) {
+        const float4 t = *reinterpret_cast<const float4*>(stage + row[it] * PITCH + 4 * (col[it] + i));
+        z[i] = t.x * c; z[i + 1] = t.y * c; z[i + 2] = t.z * c; z[i + 3] = t.w * c;
+      }
+      finish<8>(g, bias, res[it], z, y);
+      store8<OUT>(g, mm, nn / kPer, y, vec, r, st, d);
+    }
+  }
+}
+#endif  // QG_EPILOGUE
 
 // 8 E2M1 codes (one dword) times an fp16 block scale -> 8 fp16 (exact).
 __device__ inline v8h dequant8_f16(uint32_t w, _Float16 sc) {
@@ -282,6 +570,32 @@ __device__ __attribute__((always_inline)) inline void store_tiles(const GemmArgs
     }
   }
 }
+
+#if QG_EPILOGUE
+// A wave's TM x TN accumulator tiles (layout as above) through its LDS area of kWaveStage
+// bytes, 32 rows of 64 columns at a time.
+constexpr int kWavePitch = 64 * 4 + 16, kWaveStage = 32 * kWavePitch;
+template <int OUT, int TM, int TN>
+__device__ __attribute__((always_inline)) inline void store_finished(const GemmArgs& g, const v16f (&acc)[TM][TN],
+                                                                     uint8_t* stage, int mw, int nw, int lane, float c) {
+  constexpr int NJ = TN / 2;
+  uint8_t* wr = stage + (lane & 31) * kWavePitch + 16 * (lane >> 5);
+  auto put = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int qd = 0; qd < 4; ++qd) {
+        const v16f& a = acc[b / NJ][b % NJ * 2 + j];
+        *reinterpret_cast<float4*>(wr + 128 * j + 32 * qd) = make_float4(a[4 * qd], a[4 * qd + 1], a[4 * qd + 2], a[4 * qd + 3]);
+      }
+  };
+  auto at = [&](int b, int& m, int& n) __attribute__((always_inline)) {
+    m = mw + 32 * (b / NJ);
+    n = nw + 64 * (b % NJ);
+  };
+  finish_blocks<OUT, TM * NJ, 32, 64, kWavePitch>(g, stage, lane, c, put, at);
+}
+#endif
 
 // ---------------------------------------------------------------- FP8 (W8A8), few tokens
 // Four wavefronts (one per SIMD) on a (64 TM) x (64 TN) tile, each owning
@@ -427,7 +741,19 @@ __global__ void __launch_bounds__(256) k_gemm_fp8(GemmArgs g) {
     }
   }
 
+#if QG_EPILOGUE
+  // every wave is past the last barrier: the operand stages are free
+  static_assert(NS * STAGE >= 4 * kWaveStage, "a staging area per wave");
+  uint8_t* stage = smem + wave * kWaveStage;
+  const float c = *g.w_tscale * *g.a_tscale;
+  const int mw = m0 + wm * TM * 32, nw = n0 + wn * TN * 32;
+  if (g.out_mode == OUT_F32) store_finished<OUT_F32, TM, TN>(g, acc, stage, mw, nw, lane, c);
+  else if (g.out_mode == OUT_FP8) store_finished<OUT_FP8, TM, TN>(g, acc, stage, mw, nw, lane, c);
+  else if (g.out_mode == OUT_NVFP4) store_finished<OUT_NVFP4, TM, TN>(g, acc, stage, mw, nw, lane, c);
+  else store_finished<OUT_BF16, TM, TN>(g, acc, stage, mw, nw, lane, c);
+#else
   store_tiles<TM, TN>(g, acc, m0 + wm * TM * 32, n0 + wn * TN * 32, lane, *g.w_tscale * *g.a_tscale);
+#endif
 }
 
 template <int TM, int TN>
@@ -862,6 +1188,33 @@ __global__ void __launch_bounds__(64 * NW) k_gemm_splitk(GemmArgs g) {
   const float ry = out_rscale(g);
   const bool nv = g.out_mode == OUT_NVFP4;
   const float st = nv ? *g.y_scale : 0.0f, d = nv_out_d(g);
+#if QG_EPILOGUE
+  // a thread takes the columns of four outputs; the four lanes of an output 16-block
+  // are consecutive (BN / Z is a multiple of 4)
+  constexpr int Z = 4 * kPer;
+  for (int u = threadIdx.x; u < BM * (BN / Z); u += 64 * NW) {
+    const int row = u / (BN / Z), cz = u - row * (BN / Z);
+    const int m = m0 + row, n = n0 + Z * cz;
+    if (m >= g.m || n >= g.n) continue;
+    float z[Z], y[4];
+#pragma unroll
+    for (int h = 0; h < Z; h += 4) {
+      const float* p = red + row * LDR + Z * cz + h;
+      float4 sum = *reinterpret_cast<const float4*>(p);
+#pragma unroll
+      for (int w = 1; w < NRED; ++w) {
+        const float4 v = *reinterpret_cast<const float4*>(p + w * (BM * LDR));
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+      }
+      z[h] = sum.x * c; z[h + 1] = sum.y * c; z[h + 2] = sum.z * c; z[h + 3] = sum.w * c;
+    }
+    finish_at<4>(g, m, n, z, y);
+    const int no = n / kPer;
+    if (nv) store_nv_quad(g, m, no, y, st, d);
+    else store4(g, m, no, y[0], y[1], y[2], y[3], vec, ry);
+  }
+  return;
+#endif
   // the four lanes of a 16-block are consecutive (BN / 4 is a multiple of 8)
   for (int u = threadIdx.x; u < BM * (BN / 4); u += 64 * NW) {
     const int row = u / (BN / 4), c4 = u - row * (BN / 4);
@@ -1053,10 +1406,17 @@ __device__ __attribute__((always_inline)) inline void store_staged_nv(const Gemm
 // run-time branches in one kernel the register allocation of the main loop
 // suffered (W4A4 4608 x 9216 x 3072 204 -> 227 us).
 constexpr int EPI_DIRECT = 4;
+#if QG_EPILOGUE
+constexpr int EPI_FINISH = 5;  // EPI_FINISH + output mode: store_finished
+#endif
 template <int EPI, int TM, int TN>
 __device__ __attribute__((always_inline)) inline void store_tiles_epi(const GemmArgs& g, const v16f (&acc)[TM][TN],
                                                                       uint8_t* stage, int mw, int nw, int lane,
                                                                       float c) {
+#if QG_EPILOGUE
+  static_assert(EPI >= EPI_FINISH, "outputs of this translation unit");
+  store_finished<EPI - EPI_FINISH, TM, TN>(g, acc, stage, mw, nw, fresh_lane(), c);
+#else
   if constexpr (EPI == EPI_DIRECT) {
     store_tiles<TM, TN>(g, acc, mw, nw, lane, c);
   } else if constexpr (EPI == OUT_NVFP4) {
@@ -1069,8 +1429,27 @@ __device__ __attribute__((always_inline)) inline void store_tiles_epi(const Gemm
   } else {
     store_staged_as<EPI, false, TM, TN>(g, acc, stage, mw, nw, lane, c, EPI == OUT_FP8 ? out_rscale(g) : 0.0f);
   }
+#endif
 }
 
+#if QG_EPILOGUE
+#define QG_LAUNCH_EPI_NO_NVFP4(KERNEL, grid, st, g, ...)                                                          \
+  do {                                                                                                            \
+    if (g.out_mode == OUT_F32)                                                                                    \
+      hipLaunchKernelGGL((KERNEL<EPI_FINISH + OUT_F32 __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(256), 0, st, g);   \
+    else if (g.out_mode == OUT_FP8)                                                                               \
+      hipLaunchKernelGGL((KERNEL<EPI_FINISH + OUT_FP8 __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(256), 0, st, g);   \
+    else                                                                                                          \
+      hipLaunchKernelGGL((KERNEL<EPI_FINISH + OUT_BF16 __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(256), 0, st, g);  \
+  } while (0)
+#define QG_LAUNCH_EPI(KERNEL, grid, st, g, ...)                                                                   \
+  do {                                                                                                            \
+    if (g.out_mode == OUT_NVFP4)                                                                                  \
+      hipLaunchKernelGGL((KERNEL<EPI_FINISH + OUT_NVFP4 __VA_OPT__(, ) __VA_ARGS__>), grid, dim3(256), 0, st, g); \
+    else                                                                                                          \
+      QG_LAUNCH_EPI_NO_NVFP4(KERNEL, grid, st, g __VA_OPT__(, ) __VA_ARGS__);                                     \
+  } while (0)
+#else
 // The epilogue instance of an output.
 inline int epilogue_of(const GemmArgs& g) { return out_staged(g) ? g.out_mode : EPI_DIRECT; }
 // (trailing arguments: the kernel's template arguments after the epilogue)
@@ -1090,6 +1469,7 @@ inline int epilogue_of(const GemmArgs& g) { return out_staged(g) ? g.out_mode : 
     else                                                                                                          \
       QG_LAUNCH_EPI_NO_NVFP4(KERNEL, grid, st, g __VA_OPT__(, ) __VA_ARGS__);                                     \
   } while (0)
+#endif
 
 // Activation staging of the FP8 large tiles (shown for 256 rows): the rows x one
 // 128-byte chunk, read row-contiguously (8 lanes per row) and stored in LDS
@@ -1412,12 +1792,38 @@ __device__ __attribute__((always_inline)) inline void store_t288(const GemmArgs&
     }
 }
 
+#if QG_EPILOGUE
+// The same for bias, activation, residual and gate: 16 rows of 96 columns of sums at a time.
+constexpr int kT288SumPitch = 96 * 4 + 16;
+template <int OUT>
+__device__ __attribute__((always_inline)) inline void store_t288_finished(const GemmArgs& g, const v4f (&acc)[9][6],
+                                                                          uint8_t* stage, int mw, int nw, int lane, float c) {
+  uint8_t* wr = stage + (lane & 15) * kT288SumPitch + 16 * (lane >> 4);
+  auto put = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+    for (int jj = 0; jj < 6; ++jj) {
+      const v4f& a = acc[b][jj];
+      *reinterpret_cast<float4*>(wr + 64 * jj) = make_float4(a[0], a[1], a[2], a[3]);
+    }
+  };
+  auto at = [&](int b, int& m, int& n) __attribute__((always_inline)) {
+    m = mw + 16 * b;
+    n = nw;
+  };
+  finish_blocks<OUT, 9, 16, 96, kT288SumPitch>(g, stage, lane, c, put, at);
+}
+#endif
+
 template <int EPI>
 __global__ void __launch_bounds__(256) k_gemm_fp8_t288(GemmArgs g) {
   constexpr int A_STAGE = 18 * 2048;
   constexpr int RA = AStage288::RA;
   constexpr uint32_t OOB = 0x80000000u;
+#if QG_EPILOGUE
+  constexpr int OUT_STAGE = 16 * kT288SumPitch;
+#else
   constexpr int OUT_STAGE = 16 * kT288Pitch;    // output staging: 16 rows of 96 bf16 + pad
+#endif
   __shared__ __attribute__((aligned(16))) uint8_t smem[2 * A_STAGE];
   __shared__ __attribute__((aligned(16))) uint8_t sout[4 * OUT_STAGE];
 
@@ -1572,6 +1978,9 @@ __global__ void __launch_bounds__(256) k_gemm_fp8_t288(GemmArgs g) {
       }
     }
     const int mw = m0 + wm * 144, nw = n0 + wn * 96;
+#if QG_EPILOGUE
+    store_t288_finished<EPI - EPI_FINISH>(g, acc, sout + wave * OUT_STAGE, mw, nw, lane, scale);
+#else
     if constexpr (EPI != EPI_DIRECT) {
       uint8_t* st = sout + wave * OUT_STAGE;
       if (EPI == OUT_BF16 && m0 + 288 <= g.m && n0 + 192 <= g.n)
@@ -1594,6 +2003,7 @@ __global__ void __launch_bounds__(256) k_gemm_fp8_t288(GemmArgs g) {
         }
       }
     }
+#endif
   }
 }
 
@@ -2730,6 +3140,29 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
         *reinterpret_cast<float4*>(red + ((wave * MT + i) * 64 + lane) * 16 + 4 * q) =
             make_float4(acc[j][i][4 * q], acc[j][i][4 * q + 1], acc[j][i][4 * q + 2], acc[j][i][4 * q + 3]);
     __syncthreads();
+#if QG_EPILOGUE == 2
+    // a thread takes eight columns, four outputs: lanes l and l + 32 of quad q
+    for (int t = threadIdx.x; t < MT * 128; t += 64 * NW) {
+      const int i = t >> 7, l = (t >> 2) & 31, q = t & 3;
+      const int m = mb + 32 * i + l, n = (panel * NP + j) * 32 + 8 * q;
+      if (m >= g.m || n >= g.n) continue;
+      float z[8], y[4];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float* p = red + (i * 64 + l + 32 * h) * 16 + 4 * q;
+        float4 sum = *reinterpret_cast<const float4*>(p);
+#pragma unroll
+        for (int w = 1; w < NW; ++w) {
+          const float4 v = *reinterpret_cast<const float4*>(p + w * MT * 1024);
+          sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
+        }
+        z[4 * h] = sum.x * c; z[4 * h + 1] = sum.y * c; z[4 * h + 2] = sum.z * c; z[4 * h + 3] = sum.w * c;
+      }
+      finish_at<4>(g, m, n, z, y);
+      store4(g, m, n >> 1, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
+    }
+    continue;
+#endif
     for (int t = threadIdx.x; t < MT * 256; t += 64 * NW) {
       const int i = t >> 8, l = (t >> 2) & 63, q = t & 3;
       float4 sum = *reinterpret_cast<const float4*>(red + (i * 64 + l) * 16 + 4 * q);
@@ -2741,7 +3174,13 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
       const int m = mb + 32 * i + (l & 31);
       const int n = (panel * NP + j) * 32 + 8 * q + 4 * (l >> 5);
       if (m >= g.m || n >= g.n) continue;
+#if QG_EPILOGUE == 1
+      float z[4] = {sum.x * c, sum.y * c, sum.z * c, sum.w * c}, y[4];
+      finish_at<4>(g, m, n, z, y);
+      store4(g, m, n, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
+#else
       store4(g, m, n, sum.x * c, sum.y * c, sum.z * c, sum.w * c, out_vec(g), out_rscale(g));
+#endif
     }
   }
 }
@@ -2865,6 +3304,17 @@ __global__ void __launch_bounds__(64 * NWV) k_w4a16_stream(GemmArgs g) {
     compute(cb, kc0);
     if (nk == 0) {
       // panel done: lane (r, g) holds column n = 32 panel + r of rows 8 (v / 4) + 4 g + v % 4
+#if QG_EPILOGUE
+      const int nz = panel * 32 + r;
+      if (nz < g.n) {
+#pragma unroll
+        for (int v = 0; v < MV; ++v) {
+          const int m = 8 * (v >> 2) + 4 * gq + (v & 3);
+          if (m >= g.m) continue;
+          int n = nz;
+          float y = acc[v] * c;
+          if (!finish1(g, m, n, y)) continue;
+#else
       const int n = panel * 32 + r;
       if (n < g.n) {
 #pragma unroll
@@ -2872,6 +3322,7 @@ __global__ void __launch_bounds__(64 * NWV) k_w4a16_stream(GemmArgs g) {
           const int m = 8 * (v >> 2) + 4 * gq + (v & 3);
           if (m >= g.m) continue;
           const float y = acc[v] * c;
+#endif
           if (g.out_mode == OUT_F32) reinterpret_cast<float*>(g.y)[(int64_t)m * g.ldy + n] = y;
           else reinterpret_cast<uint16_t*>(g.y)[(int64_t)m * g.ldy + n] = (uint16_t)pk_bf16(y, 0.0f);
         }
@@ -2976,10 +3427,17 @@ __global__ void __launch_bounds__(512, 4) k_w4a16_gemv(GemmArgs g) {
     cur ^= 1;
     if (nk == 0) {
       // panel done: row r's two halves sit in lanes r and r + 32
+#if QG_EPILOGUE
+      float v = (acc + __shfl_xor(acc, 32)) * c;
+      acc = 0.0f;
+      int n = panel * 32 + r;
+      if (gq == 0 && n < g.n && finish1(g, 0, n, v)) {
+#else
       const float v = (acc + __shfl_xor(acc, 32)) * c;
       acc = 0.0f;
       const int n = panel * 32 + r;
       if (gq == 0 && n < g.n) {
+#endif
         if (g.out_mode == OUT_F32) reinterpret_cast<float*>(g.y)[n] = v;
         else reinterpret_cast<uint16_t*>(g.y)[n] = (uint16_t)pk_bf16(v, 0.0f);
       }
@@ -2989,6 +3447,34 @@ __global__ void __launch_bounds__(512, 4) k_w4a16_gemv(GemmArgs g) {
   }
 }
 
+#if QG_EPILOGUE
+// k = 0: the sums are zeros, the rest of the epilogue stays. A thread per 16 outputs.
+__global__ void __launch_bounds__(256) k_finish_rows(GemmArgs g) {
+  const int blocks = g.n / (16 * kPer);
+  const float r = out_rscale(g), st = g.out_mode == OUT_NVFP4 ? *g.y_scale : 0.0f, d = nv_out_d(g);
+  for (int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x; t < (int64_t)g.m * blocks; t += (int64_t)gridDim.x * 256) {
+    const int m = (int)(t / blocks), n = 16 * (int)(t - (int64_t)m * blocks);
+    float y[16];
+    for (int h = 0; h < 16; h += 4) {
+      float z[4 * kPer] = {}, y4[4];
+      finish_at<4>(g, m, (n + h) * kPer, z, y4);
+      for (int i = 0; i < 4; ++i) y[h + i] = y4[i];
+    }
+    if (g.out_mode != OUT_NVFP4) {
+      for (int h = 0; h < 16; h += 4) store4(g, m, n + h, y[h], y[h + 1], y[h + 2], y[h + 3], false, r);
+      continue;
+    }
+    uint32_t am = 0;
+    for (int i = 0; i < 16; ++i) am = max(am, f2u(y[i]) & 0x7FFFFFFFu);
+    float rb;
+    g.y_bscale[(int64_t)m * (g.ldy >> 4) + (n >> 4)] = (uint8_t)nv_block(am, st, d, rb);
+    for (int i = 0; i < 16; ++i) y[i] = __fmul_rn(y[i], rb);
+    uint32_t* o = reinterpret_cast<uint32_t*>(reinterpret_cast<uint8_t*>(g.y) + (int64_t)m * (g.ldy >> 1) + (n >> 1));
+    o[0] = hw_e2m1x8(y);
+    o[1] = hw_e2m1x8(y + 8);
+  }
+}
+#else
 // k = 0: every output is zero (NVFP4: zero codes and zero block scales, one
 // thread per code byte at a time). A launch of 2^32 threads or more is cut off
 // without an error, so the grid is bounded and walks the outputs.
@@ -3009,6 +3495,7 @@ inline void zero_rows(void* y, uint8_t* y_bscale, int64_t m, int64_t n, int64_t 
   hipLaunchKernelGGL(k_zero_rows, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, st, y, y_bscale, m,
                      n, ldy, out_mode);
 }
+#endif
 
 template <int MT, int NP, int NW, int D, bool XLDS>
 static hipError_t run_w4a16_splitk(GemmArgs g, hipStream_t st) {
@@ -3083,15 +3570,10 @@ static hipError_t launch_mx(GemmArgs g, hipStream_t st) {
   return launch_large<MODE>(g, cus, st);
 }
 
-hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale,
-                       int64_t lda, const uint8_t* w_packed, int64_t m, int64_t n, int64_t k,
-                       void* y, int64_t ldy, int out_mode, const float* y_scale, uint8_t* y_bscale,
-                       hipStream_t st) {
-  if (m == 0 || n == 0) return hipSuccess;
-  if (k == 0) {
-    zero_rows(y, y_bscale, m, n, ldy, out_mode, st);
-    return hipGetLastError();
-  }
+// The arguments of a product with an [n, k] weight.
+static GemmArgs gemm_args(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale, int64_t lda,
+                          const uint8_t* w_packed, int64_t m, int64_t n, int64_t k, void* y, int64_t ldy, int out_mode,
+                          const float* y_scale, uint8_t* y_bscale) {
   const int w_fmt = (a_fmt == 1 || a_fmt == 3 || a_fmt == 4) ? a_fmt : 2;
   GemmArgs g;
   g.a = reinterpret_cast<const uint8_t*>(a);
@@ -3110,6 +3592,13 @@ hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const 
   g.y_scale = y_scale;
   g.y_bscale = y_bscale;
   g.tiles_m = g.tiles_n = 0;
+  return g;
+}
+
+// The kernel of a product with m, n, k > 0.
+static hipError_t launch_product(int a_fmt, GemmArgs g, hipStream_t st) {
+  const int64_t m = g.m, n = g.n, k = g.k;
+  const int out_mode = g.out_mode;
   if (a_fmt == 3) return launch_mx<MODE_MXFP4>(g, st);
   if (a_fmt == 4) return launch_mx<MODE_MXFP8>(g, st);
   const int cus = device_cus();
@@ -3189,6 +3678,35 @@ hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const 
   }
 }
 
+#if QG_EPILOGUE
+hipError_t launch(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale, int64_t lda,
+                  const uint8_t* w_packed, int64_t m, int64_t n, int64_t k, const Epilogue& e, void* y, int64_t ldy,
+                  int out_mode, const float* y_scale, uint8_t* y_bscale, hipStream_t st) {
+  if (m == 0 || n == 0) return hipSuccess;
+  GemmArgs g = gemm_args(a_fmt, a, a_bscale, a_tscale, lda, w_packed, m, n, k, y, ldy, out_mode, y_scale, y_bscale);
+  g.e = e;
+  // eight elements in one load (fp32 two): a row's pieces start at multiples of eight
+  g.e.bias_vec = reinterpret_cast<uintptr_t>(e.bias) % 16 == 0;
+  g.e.res_vec = reinterpret_cast<uintptr_t>(e.residual) % 16 == 0 && e.ldr * (e.res_f32 ? 4 : 2) % 16 == 0;
+  if (k > 0) return launch_product(a_fmt, g, st);
+  const int64_t groups = (m * (n / 16) + 255) / 256;
+  hipLaunchKernelGGL(k_finish_rows, dim3((unsigned)std::min<int64_t>(groups, 65536)), dim3(256), 0, st, g);
+  return hipGetLastError();
+}
+#else
+hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale,
+                       int64_t lda, const uint8_t* w_packed, int64_t m, int64_t n, int64_t k,
+                       void* y, int64_t ldy, int out_mode, const float* y_scale, uint8_t* y_bscale,
+                       hipStream_t st) {
+  if (m == 0 || n == 0) return hipSuccess;
+  if (k == 0) {
+    zero_rows(y, y_bscale, m, n, ldy, out_mode, st);
+    return hipGetLastError();
+  }
+  return launch_product(a_fmt, gemm_args(a_fmt, a, a_bscale, a_tscale, lda, w_packed, m, n, k, y, ldy, out_mode, y_scale,
+                                         y_bscale), st);
+}
+
 // The FP8 decode scale of a small bf16 activation alone (one workgroup):
 // the degenerate shapes of the fused linear, which launch no GEMM tile.
 __global__ void __launch_bounds__(256) k_fp8_scale_only(const uint16_t* __restrict__ x, int64_t m, int64_t k,
@@ -3242,5 +3760,9 @@ hipError_t launch_linear_fp8(const uint16_t* x, int64_t ldx, float* a_tscale, co
   if (rows32 * ((n + 127) / 128) <= cus) return run_splitk<MODE_FP8, 1, 4, 8, 1, true>(g, st);
   return run_splitk<MODE_FP8, 1, 2, 4, 2, true>(g, st);
 }
+#endif  // QG_EPILOGUE
 
+#if QG_EPILOGUE
+}  // namespace fused, namespace gated
+#endif
 }  // namespace qg

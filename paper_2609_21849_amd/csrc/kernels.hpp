@@ -51,6 +51,47 @@ hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const 
                        int64_t lda, const uint8_t* w_packed, int64_t m, int64_t n, int64_t k,
                        void* y, int64_t ldy, int out_mode, const float* y_scale, uint8_t* y_bscale,
                        hipStream_t st);
+// What qg_gemm_fused does with the sums: bias [n], activation (qg_activation),
+// residual [m, ldr]; bf16 or fp32. The *_vec are the launcher's: aligned for wide loads.
+struct Epilogue {
+  const void* bias;
+  const void* residual;
+  int64_t ldr;
+  int act;
+  bool bias_f32, bias_vec, res_f32, res_vec;
+};
+// launch_gemm with that epilogue (out_mode as there). gated: rows 2 i and 2 i + 1 of
+// the [n, k] weight are output i's gate and up rows; y has n / 2 columns, no residual.
+namespace fused {
+hipError_t launch(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale, int64_t lda,
+                  const uint8_t* w_packed, int64_t m, int64_t n, int64_t k, const Epilogue& e, void* y, int64_t ldy,
+                  int out_mode, const float* y_scale, uint8_t* y_bscale, hipStream_t st);
+}
+namespace gated {
+hipError_t launch(int a_fmt, const void* a, const uint8_t* a_bscale, const float* a_tscale, int64_t lda,
+                  const uint8_t* w_packed, int64_t m, int64_t n, int64_t k, const Epilogue& e, void* y, int64_t ldy,
+                  int out_mode, const float* y_scale, uint8_t* y_bscale, hipStream_t st);
+}
+// Residual addition, RMS norm and quantization (qg_rms_norm).
+struct NormArgs {
+  const uint16_t* x;
+  int64_t ldx;
+  const uint16_t* res;  // may be null
+  int64_t ldr;
+  const void* w;        // weight [cols], bf16 or fp32
+  bool w_f32;
+  float eps;
+  int64_t rows;
+  int cols;
+  uint16_t* sum;        // bf16(x + res) [rows, lds], may be null
+  int64_t lds;
+  uint8_t* y;           // bf16 [rows, ldy] or codes (dense)
+  int64_t ldy;
+  uint8_t* bscale;
+  float* tscale;        // FP8, NVFP4: read (static) or written
+  uint32_t* partial;    // the launcher's
+};
+hipError_t launch_rms_norm(int fmt, const NormArgs& a, bool static_scale, hipStream_t st);
 // W8A8 linear from bf16 activations x [m, ldx] (16-byte aligned rows):
 // the dynamic FP8 quantization of x inside the split-K GEMM; a_tscale
 // receives the decode scale; out_mode 0 (bf16) or 1 (fp32)

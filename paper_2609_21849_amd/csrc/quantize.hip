@@ -559,26 +559,6 @@ __global__ void __launch_bounds__(256) k_quant_slots(const uint16_t* __restrict_
 // block are units 4 j .. 4 j + 3 of the tensor and lanes 4 j .. 4 j + 3 of one
 // wave, which share its max with two lane swaps.
 
-// E8M0 code of a block from the fp32 bits of its largest magnitude and the
-// factor its elements are multiplied by.
-template <bool FP4>
-__device__ inline uint32_t mx_block(uint32_t am, float& r) {
-  // floor(log2(max)) from the fp32 bits (normal or denormal), then the code.
-  // A block holding inf or NaN gets the E8M0 NaN code 255 (its element codes
-  // are then unspecified: r = 0 makes them signed zeros).
-  int e = 0;
-  if (am >= 0x7F800000u) {
-    e = 255;
-  } else if (am != 0u) {
-    const int ef = (int)(am >> 23);
-    const int fl = (ef > 0) ? ef - 127 : (31 - __builtin_clz(am)) - 149;
-    e = min(max(fl - (FP4 ? 2 : 8) + 127, 0), 254);
-  }
-  // 2^(127 - e); finite bf16 inputs give e <= 252, so this is a normal number
-  r = (e == 255) ? 0.0f : u2f((uint32_t)(254 - e) << 23);
-  return (uint32_t)e;
-}
-
 // 16-byte aligned rows. Each lane codes H half blocks of 16 elements, 64 apart
 // (two adjacent 16-byte loads each, all issued before the first is used); a lane
 // pair shares a block's max. Codes and scales are contiguous in unit order, so

@@ -1,0 +1,433 @@
+// rmsnorm.hip -- residual addition, root-mean-square norm and quantization of its
+// result in one pass (gfx950): what stands in front of a quantized linear.
+//
+//   h = bf16(x + residual)                       (h = x without a residual)
+//   y_j = fl(fl(h_j r) w_j), r = fl(1 / fl(sqrt(fl(mean_j h_j^2) + eps)))
+//   y as bf16, or quantized from its fp32 values: FP8, NVFP4, MXFP4, MXFP8
+//
+// The norm is that of the stored sum h, so what a caller keeps and what was normed
+// are the same numbers, and y can be computed again from h. The squares are summed
+// in fp32, a thread's own first, then over the lanes and waves in a fixed order.
+//
+// HBM-bound: x and the residual are read once, h and y written once. A row stays in
+// the registers of the threads that share it (packed bf16, 16 elements a unit: a whole
+// NVFP4 block, half an MX one, and a 16-byte store of FP8 codes), from the loads to the
+// codes. Rows of any alignment and length: whole units are loaded with wide loads
+// that need no alignment, a shorter last one element by element.
+//
+// A tensor scale taken from y (dynamic FP8, NVFP4) needs the largest |y| of all
+// rows before the first code: one workgroup does a tensor of few rows in one launch;
+// otherwise the first launch writes h and a maximum per workgroup (parked in the
+// code buffer that the last one overwrites), the second makes the scale of them, the
+// third norms h again, with the same steps, and codes it.
+#include <algorithm>
+
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace qg {
+
+enum { F_BF16 = 0, F_FP8 = 1, F_NVFP4 = 2, F_MXFP4 = 3, F_MXFP8 = 4, F_AMAX = 5 };  // qg_format; F_AMAX: h and max |y| alone
+
+// ---------------------------------------------------------------- 16 elements of a row
+// cnt (from the unit's first to the row's last element) >= 16: whole.
+__device__ __attribute__((always_inline)) inline void load16(const uint16_t* p, int cnt, uint32_t (&w)[8]) {
+  if (cnt >= 16) {
+    __builtin_memcpy(w, p, 32);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const uint32_t lo = (2 * i < cnt) ? (uint32_t)p[2 * i] : 0u;
+      const uint32_t hi = (2 * i + 1 < cnt) ? (uint32_t)p[2 * i + 1] : 0u;
+      w[i] = lo | (hi << 16);
+    }
+  }
+}
+__device__ __attribute__((always_inline)) inline void store16(uint16_t* p, int cnt, const uint32_t (&w)[8]) {
+  if (cnt >= 16) {
+    __builtin_memcpy(p, w, 32);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (i < cnt) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
+  }
+}
+
+__device__ __attribute__((always_inline)) inline void load_weight(const NormArgs& a, int c, int cnt, float (&v)[16]) {
+  if (a.w_f32) {
+    const float* p = reinterpret_cast<const float*>(a.w) + c;
+    if (cnt >= 16) {
+      __builtin_memcpy(v, p, 64);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = (i < cnt) ? p[i] : 0.0f;
+    }
+  } else {
+    uint32_t w[8];
+    load16(reinterpret_cast<const uint16_t*>(a.w) + c, cnt, w);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      v[2 * i] = bf16_lo(w[i]);
+      v[2 * i + 1] = bf16_hi(w[i]);
+    }
+  }
+}
+
+// A unit of h; with a residual the sum, written to a.sum where the caller wants it.
+__device__ __attribute__((always_inline)) inline void load_h(const NormArgs& a, int64_t row, int c, int cnt, uint32_t (&h)[8]) {
+  load16(a.x + row * a.ldx + c, cnt, h);
+  if (a.res) {
+    uint32_t r[8];
+    load16(a.res + row * a.ldr + c, cnt, r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) h[i] = pk_bf16(bf16_lo(h[i]) + bf16_lo(r[i]), bf16_hi(h[i]) + bf16_hi(r[i]));
+    if (a.sum) store16(a.sum + row * a.lds + c, cnt, h);
+  }
+}
+
+__device__ __attribute__((always_inline)) inline float squares(const uint32_t (&h)[8], float ss, float scale) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float lo = bf16_lo(h[i]) * scale, hi = bf16_hi(h[i]) * scale;
+    ss = __builtin_fmaf(lo, lo, ss);
+    ss = __builtin_fmaf(hi, hi, ss);
+  }
+  return ss;
+}
+
+__device__ __attribute__((always_inline)) inline void norm16(const uint32_t (&h)[8], const float (&w)[16], float pre, float rstd,
+                                                             float (&y)[16]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    y[2 * i] = __fmul_rn(__fmul_rn(bf16_lo(h[i]) * pre, rstd), w[2 * i]);
+    y[2 * i + 1] = __fmul_rn(__fmul_rn(bf16_hi(h[i]) * pre, rstd), w[2 * i + 1]);
+  }
+}
+
+__device__ __attribute__((always_inline)) inline uint32_t amax16(const float (&y)[16]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max(m, f2u(y[i]) & 0x7FFFFFFFu);
+  return m;
+}
+
+// Elements [c, c + 16) of row `row` of y, `cnt` of them in the row, in the output
+// format. s: tensor scale; r: its reciprocal (FP8). MX: the lanes of units 2 j and 2 j + 1
+// call this together. NVFP4 and MX rows are whole blocks.
+template <int FMT>
+__device__ __attribute__((always_inline)) inline void store_y(const NormArgs& a, int64_t row, int c, int cnt, const float (&y)[16],
+                                                              float s, float r) {
+  if constexpr (FMT == F_BF16) {
+    uint32_t w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) w[i] = pk_bf16(y[2 * i], y[2 * i + 1]);
+    store16(reinterpret_cast<uint16_t*>(a.y) + row * a.ldy + c, cnt, w);
+  } else if constexpr (FMT == F_FP8 || FMT == F_MXFP8) {
+    if constexpr (FMT == F_MXFP8) {
+      uint32_t am = amax16(y);
+      am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+      const uint32_t e = mx_block<false>(am, r);
+      if ((c & 31) == 0) a.bscale[row * (a.cols >> 5) + (c >> 5)] = (uint8_t)e;
+    }
+    uint32_t q[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float t[4] = {__fmul_rn(y[4 * i], r), __fmul_rn(y[4 * i + 1], r), __fmul_rn(y[4 * i + 2], r),
+                          __fmul_rn(y[4 * i + 3], r)};
+      q[i] = hw_e4m3x4(t);
+    }
+    uint8_t* o = a.y + row * a.cols + c;
+    if (cnt >= 16) {
+      __builtin_memcpy(o, q, 16);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (i < cnt) o[i] = (uint8_t)(q[i >> 2] >> (8 * (i & 3)));
+    }
+  } else {
+    uint32_t am = amax16(y);
+    if constexpr (FMT == F_MXFP4) {
+      am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+      const uint32_t e = mx_block<true>(am, r);
+      if ((c & 31) == 0) a.bscale[row * (a.cols >> 5) + (c >> 5)] = (uint8_t)e;
+    } else {
+      a.bscale[row * (a.cols >> 4) + (c >> 4)] = (uint8_t)nv_block(am, s, __fmul_rn(6.0f, s), r);
+    }
+    float t[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t[i] = __fmul_rn(y[i], r);
+    const uint32_t q[2] = {hw_e2m1x8(t), hw_e2m1x8(t + 8)};
+    __builtin_memcpy(a.y + row * (a.cols >> 1) + (c >> 1), q, 8);
+  }
+}
+
+// ---------------------------------------------------------------- reductions
+__device__ __attribute__((always_inline)) inline float wave_sum(float v) {
+  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+__device__ __attribute__((always_inline)) inline uint32_t wave_max(uint32_t v) {
+  for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
+  return v;
+}
+
+// Over the TPR threads of a row, the whole workgroup if more than a wave; red: words
+// that no thread still reads.
+template <int TPR>
+__device__ __attribute__((always_inline)) inline float row_sum(float v, float* red) {
+  v = wave_sum(v);
+  if constexpr (TPR > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = red[0];
+#pragma unroll
+    for (int i = 1; i < TPR / 64; ++i) v += red[i];
+  }
+  return v;
+}
+
+// Over the whole workgroup.
+__device__ __attribute__((always_inline)) inline uint32_t group_max(uint32_t v) {
+  __shared__ uint32_t part[16];
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0;
+  for (int i = 0; i < (int)(blockDim.x >> 6); ++i) v = max(v, part[i]);
+  return v;
+}
+
+// Squares of elements past 2^64 leave fp32: such a row (a sum that is no finite
+// number) is summed again times 2^-96, an exact factor, which its elements get too.
+constexpr float kHugeScale = 1.262177448353618888658765e-29f;  // 2^-96
+
+__device__ __attribute__((always_inline)) inline float rstd_of(float ss, int cols, float eps) {
+  const float v = __fadd_rn(__fdiv_rn(ss, (float)cols), eps);
+  return v > 0.0f || v != v ? __fdiv_rn(1.0f, __fsqrt_rn(v)) : 0.0f;  // (a row of zeros with eps = 0)
+}
+
+__device__ __attribute__((always_inline)) inline float scale_of_max(uint32_t m, float divisor) {
+  return m >= 0x7F800000u ? __builtin_nanf("") : __fdiv_rn(u2f(m), divisor);
+}
+
+// ---------------------------------------------------------------- rows in registers
+// TPR threads share a row, NV units of 16 elements each: unit t + TPR i. TPR = 64: a
+// workgroup has a row per wave at a time, else one row. DYN: the workgroup holds every
+// row of the tensor, so its largest |y| gives the tensor scale, which it writes.
+template <int FMT, int NV, int TPR, bool DYN>
+__global__ void __launch_bounds__(DYN || TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs a) {
+  __shared__ float red[2][16];
+  const int t = (int)threadIdx.x % TPR, rpb = (int)blockDim.x / TPR;
+  const float divisor = FMT == F_FP8 ? 448.0f : 2688.0f;
+  float s = 0.0f, r = 0.0f;
+  if ((FMT == F_FP8 || FMT == F_NVFP4) && !DYN) {
+    s = *a.tscale;
+    r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
+  }
+  uint32_t am = 0;
+  int turn = 0;
+  for (int64_t row = (int64_t)blockIdx.x * rpb + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * rpb) {
+    uint32_t h[NV][8];
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = 16 * (t + TPR * i);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[i][j] = 0u;
+      if (c < a.cols) load_h(a, row, c, a.cols - c, h[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, 1.0f);
+    ss = row_sum<TPR>(ss, red[turn]);
+    turn ^= 1;
+    float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
+    if (!(ss <= 3.40282347e38f)) {  // the same in every thread of the row
+      pre = kHugeScale;
+      ss = 0.0f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, pre);
+      rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, 0.0f);
+      turn ^= 1;
+    }
+    if constexpr (FMT == F_AMAX || DYN) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = 16 * (t + TPR * i);
+        if (c >= a.cols) continue;
+        float w[16], y[16];
+        load_weight(a, c, a.cols - c, w);
+        norm16(h[i], w, pre, rstd, y);
+        am = max(am, amax16(y));
+      }
+    }
+    if constexpr (DYN) {  // one turn of the loop: every row of the tensor is here
+      s = scale_of_max(group_max(am), divisor);
+      r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
+      if (threadIdx.x == 0) *a.tscale = s;
+    }
+    if constexpr (FMT != F_AMAX) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = 16 * (t + TPR * i);
+        if (c >= a.cols) continue;
+        float w[16], y[16];
+        load_weight(a, c, a.cols - c, w);
+        norm16(h[i], w, pre, rstd, y);
+        store_y<FMT>(a, row, c, a.cols - c, y, s, r);
+      }
+    }
+  }
+  if constexpr (FMT == F_AMAX) {
+    am = group_max(am);
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = am;
+  }
+}
+
+// Rows too long for the registers: a workgroup walks the row twice (three times
+// where the squares overflow), the second time from the caches where it fits.
+template <int FMT>
+__global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
+  __shared__ float red[2][16];
+  float s = 0.0f, r = 0.0f;
+  if (FMT == F_FP8 || FMT == F_NVFP4) {
+    s = *a.tscale;
+    r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
+  }
+  uint32_t am = 0;
+  NormArgs again = a;  // the second reading: of the stored sum where there is one
+  if (a.res && a.sum) {
+    again.x = a.sum;
+    again.ldx = a.lds;
+    again.res = nullptr;
+  }
+  again.sum = nullptr;
+  int turn = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    uint32_t h[8];
+    float ss = 0.0f;
+    for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
+      load_h(a, row, (int)c, (int)min((int64_t)16, a.cols - c), h);
+      ss = squares(h, ss, 1.0f);
+    }
+    ss = row_sum<1024>(ss, red[turn]);
+    turn ^= 1;
+    float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
+    if (!(ss <= 3.40282347e38f)) {
+      pre = kHugeScale;
+      ss = 0.0f;
+      for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
+        load_h(again, row, (int)c, (int)min((int64_t)16, a.cols - c), h);
+        ss = squares(h, ss, pre);
+      }
+      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, 0.0f);
+      turn ^= 1;
+    }
+    for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
+      const int cnt = (int)min((int64_t)16, a.cols - c);
+      float w[16], y[16];
+      load_h(again, row, (int)c, cnt, h);
+      load_weight(a, (int)c, cnt, w);
+      norm16(h, w, pre, rstd, y);
+      if constexpr (FMT == F_AMAX) am = max(am, amax16(y));
+      else store_y<FMT>(a, row, (int)c, cnt, y, s, r);
+    }
+  }
+  if constexpr (FMT == F_AMAX) {
+    am = group_max(am);
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = am;
+  }
+}
+
+// The tensor scale from `count` maxima (fp32 bits), which may lie in `scale` itself.
+__global__ void __launch_bounds__(256) k_norm_scale(const uint32_t* partial, int count, float* scale, float divisor) {
+  uint32_t m = 0;
+  for (int i = (int)threadIdx.x; i < count; i += 256) m = max(m, partial[i]);
+  m = group_max(m);
+  if (threadIdx.x == 0) *scale = scale_of_max(m, divisor);
+}
+
+__global__ void k_norm_empty(float* scale) { *scale = 0.0f; }
+
+// ---------------------------------------------------------------- launchers
+constexpr int64_t kNormGroups = 2048;  // eight workgroups of 256 threads a CU
+
+// Threads that share a row of `units` 16-element units (0: too long for registers).
+static int threads_per_row(int64_t units) {
+  return units <= 64 * 4 ? 64 : units <= 256 * 4 ? 256 : units <= 1024 * 4 ? 1024 : 0;
+}
+
+template <int FMT, bool DYN>
+static void launch_rows(const NormArgs& a, int tpr, unsigned groups, unsigned threads, hipStream_t st) {
+  const int64_t units = ((int64_t)a.cols + 15) / 16;
+  const int nv = tpr ? (int)((units + tpr - 1) / tpr) : 0;
+#define QG_NORM(NV, TPR) hipLaunchKernelGGL((k_rms_norm<FMT, NV, TPR, DYN>), dim3(groups), dim3(threads), 0, st, a)
+#define QG_NORM_NV(TPR)                                                                            \
+  do {                                                                                             \
+    if (nv == 1) QG_NORM(1, TPR);                                                                  \
+    else if (nv == 2) QG_NORM(2, TPR);                                                             \
+    else if (nv == 3) QG_NORM(3, TPR);                                                             \
+    else QG_NORM(4, TPR);                                                                          \
+  } while (0)
+  if (tpr == 64) QG_NORM_NV(64);
+  else if (tpr == 256) QG_NORM_NV(256);
+  else if (tpr == 1024) QG_NORM_NV(1024);
+  else if constexpr (!DYN) hipLaunchKernelGGL((k_rms_norm_long<FMT>), dim3(groups), dim3(1024), 0, st, a);
+#undef QG_NORM_NV
+#undef QG_NORM
+}
+
+template <int FMT>
+static void launch_all(const NormArgs& a, int64_t groups_max, hipStream_t st) {
+  const int tpr = threads_per_row(((int64_t)a.cols + 15) / 16);
+  const int64_t rpb = tpr == 64 ? 4 : 1;
+  const unsigned groups = (unsigned)std::min<int64_t>((a.rows + rpb - 1) / rpb, groups_max);
+  launch_rows<FMT, false>(a, tpr, groups, tpr == 64 ? 256 : tpr ? tpr : 1024, st);
+}
+
+// A tensor scale taken from y.
+template <int FMT>
+static hipError_t launch_dynamic(NormArgs a, hipStream_t st) {
+  const int tpr = threads_per_row(((int64_t)a.cols + 15) / 16);
+  if ((tpr == 64 && a.rows <= 16) || (tpr != 0 && a.rows == 1)) {
+    launch_rows<FMT, true>(a, tpr, 1, (unsigned)(a.rows * tpr), st);
+    return hipGetLastError();
+  }
+  const int64_t bytes = FMT == F_FP8 ? a.rows * a.cols : a.rows * a.cols / 2;
+  const uintptr_t base = (reinterpret_cast<uintptr_t>(a.y) + 3) & ~uintptr_t(3);
+  const int64_t cap = (bytes - (int64_t)(base - reinterpret_cast<uintptr_t>(a.y))) / 4;
+  const int64_t rpb = tpr == 64 ? 4 : 1;
+  int64_t groups = std::min<int64_t>((a.rows + rpb - 1) / rpb, kNormGroups);
+  a.partial = reinterpret_cast<uint32_t*>(base);
+  if (groups > cap) {  // short rows: one workgroup, its maximum straight into the scale's place
+    groups = 1;
+    a.partial = reinterpret_cast<uint32_t*>(a.tscale);
+  }
+  launch_all<F_AMAX>(a, groups, st);
+  hipLaunchKernelGGL(k_norm_scale, dim3(1), dim3(256), 0, st, a.partial, (int)groups, a.tscale, FMT == F_FP8 ? 448.0f : 2688.0f);
+  if (a.res && a.sum) {
+    a.x = a.sum;
+    a.ldx = a.lds;
+    a.res = nullptr;
+  }
+  a.sum = nullptr;
+  launch_all<FMT>(a, kNormGroups, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_rms_norm(int fmt, const NormArgs& a, bool static_scale, hipStream_t st) {
+  if (a.rows == 0 || a.cols == 0) {
+    if (static_scale || !a.tscale) return hipSuccess;
+    hipLaunchKernelGGL(k_norm_empty, dim3(1), dim3(1), 0, st, a.tscale);
+    return hipGetLastError();
+  }
+  if (fmt == F_FP8 && !static_scale) return launch_dynamic<F_FP8>(a, st);
+  if (fmt == F_NVFP4 && !static_scale) return launch_dynamic<F_NVFP4>(a, st);
+  if (fmt == F_FP8) launch_all<F_FP8>(a, kNormGroups, st);
+  else if (fmt == F_NVFP4) launch_all<F_NVFP4>(a, kNormGroups, st);
+  else if (fmt == F_MXFP4) launch_all<F_MXFP4>(a, kNormGroups, st);
+  else if (fmt == F_MXFP8) launch_all<F_MXFP8>(a, kNormGroups, st);
+  else launch_all<F_BF16>(a, kNormGroups, st);
+  return hipGetLastError();
+}
+
+}  // namespace qg
