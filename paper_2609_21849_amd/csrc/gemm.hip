@@ -211,23 +211,49 @@ __device__ __attribute__((always_inline)) inline void store_nv_quad(const GemmAr
 //   SiLU       z / (1 + e^-z)
 //   GELU tanh  z / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3): 0.5 (1 + tanh u) is
 //              the logistic function of 2 u
-//   GELU erf   z erfc(-z / sqrt 2) / 2, without the cancellation of 1 + erf at z < 0
+//   GELU erf   z Phi(z), Phi(-x) = exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.3 x / sqrt 2), x >= 0: the
+//              scaled tail erfcx / 2 as a polynomial of degree 8 in t without a constant
+//              term, least in its largest relative error (2e-8; fitted by reweighted
+//              least squares over x / sqrt 2 in [0, 9.5]); no cancellation at z < 0
 // Far negative z: the exponential is inf, its reciprocal 0, the result -0.
 __device__ __attribute__((always_inline)) inline float logistic(float t) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504f));
+}
+
+__device__ __attribute__((always_inline)) inline float normal_cdf(float z) {
+  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.21213203f, __builtin_fabsf(z), 1.0f));
+  float p = -0.06471703946590424f;
+  p = __builtin_fmaf(p, t, 0.24254822731018066f);
+  p = __builtin_fmaf(p, t, -0.2556132376194f);
+  p = __builtin_fmaf(p, t, 0.2731975317001343f);
+  p = __builtin_fmaf(p, t, -0.046815626323223114f);
+  p = __builtin_fmaf(p, t, 0.10721813887357712f);
+  p = __builtin_fmaf(p, t, 0.07424121350049973f);
+  p = __builtin_fmaf(p, t, 0.08534596860408783f);
+  p = __builtin_fmaf(p, t, 0.08459480851888657f);
+  const float tail = t * p * __builtin_amdgcn_exp2f(z * z * -0.72134752f);
+  return z < 0.0f ? tail : 1.0f - tail;
+}
+
+template <int ACT>
+__device__ __attribute__((always_inline)) inline float activated(float z) {
+  if constexpr (ACT == QG_ACT_SILU) return z * logistic(z);
+  else if constexpr (ACT == QG_ACT_GELU_TANH) return z * logistic(1.59576912f * z * __builtin_fmaf(0.044715f * z, z, 1.0f));
+  else if constexpr (ACT == QG_ACT_GELU_ERF) return z * normal_cdf(z);
+  else return z;
 }
 
 template <int W>
 __device__ __attribute__((always_inline)) inline void activate(float (&v)[W], int act) {
   if (act == QG_ACT_SILU) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] *= logistic(v[i]);
+    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_SILU>(v[i]);
   } else if (act == QG_ACT_GELU_TANH) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] *= logistic(1.59576912f * v[i] * (1.0f + 0.044715f * v[i] * v[i]));
+    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_GELU_TANH>(v[i]);
   } else if (act == QG_ACT_GELU_ERF) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] *= 0.5f * erfcf(-0.70710678f * v[i]);
+    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_GELU_ERF>(v[i]);
   }
 }
 
@@ -286,31 +312,20 @@ __device__ __attribute__((always_inline)) inline void add_run(float* v, const Ru
 // Weight rows, so accumulator columns, of one output.
 constexpr int kPer = kGated ? 2 : 1;
 
-// The bias of kPer W weight rows and the residual of W outputs.
+// W outputs m, n / kPer on from the scaled sums z of kPer W consecutive weight rows
+// from n on, with their bias and residual.
 template <int W>
-struct BiasRun {
-  Run<W> t[kPer];
-};
-template <int W>
-__device__ __attribute__((always_inline)) inline BiasRun<W> load_bias(const GemmArgs& g, int n) {
-  BiasRun<W> b;
-#pragma unroll
-  for (int h = 0; h < kPer; ++h) b.t[h] = load_run<W>(g.e.bias, n + h * W, g.e.bias_f32, g.e.bias_vec);
-  return b;
-}
-template <int W>
-__device__ __attribute__((always_inline)) inline Run<W> load_residual(const GemmArgs& g, int m, int n) {
-  return load_run<W>(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32, g.e.res_vec);
-}
-
-// W outputs from the scaled sums z of kPer W consecutive weight rows, with their
-// bias and residual (read only where g.e has them).
-template <int W>
-__device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, const BiasRun<W>& b, const Run<W>& res,
-                                                             float (&z)[kPer * W], float (&y)[W]) {
+__device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, int m, int n, float (&z)[kPer * W],
+                                                             float (&y)[W]) {
+  Run<W> b[kPer], res;
   if (g.e.bias) {
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) add_run<W>(z + h * W, b.t[h], g.e.bias_f32);
+    for (int h = 0; h < kPer; ++h) b[h] = load_run<W>(g.e.bias, n + h * W, g.e.bias_f32, g.e.bias_vec);
+  }
+  if (!kGated && g.e.residual) res = load_run<W>(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32, g.e.res_vec);
+  if (g.e.bias) {
+#pragma unroll
+    for (int h = 0; h < kPer; ++h) add_run<W>(z + h * W, b[h], g.e.bias_f32);
   }
 #pragma unroll
   for (int i = 0; i < W; ++i) y[i] = z[kPer * i];
@@ -321,17 +336,6 @@ __device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, 
   } else if (g.e.residual) {
     add_run<W>(y, res, g.e.res_f32);
   }
-}
-
-// The same, loading both: outputs m, n / kPer on for weight rows from n on.
-template <int W>
-__device__ __attribute__((always_inline)) inline void finish_at(const GemmArgs& g, int m, int n, float (&z)[kPer * W],
-                                                                float (&y)[W]) {
-  BiasRun<W> b = {};
-  Run<W> res = {};
-  if (g.e.bias) b = load_bias<W>(g, n);
-  if (!kGated && g.e.residual) res = load_residual<W>(g, m, n);
-  finish<W>(g, b, res, z, y);
 }
 
 // One output from the scaled sum of one column held by each lane (the weight-pool
@@ -356,48 +360,74 @@ __device__ __attribute__((always_inline)) inline bool finish1(const GemmArgs& g,
   return true;
 }
 
-// Eight consecutive outputs y[m][n .. n+7] (n % 8 == 0) in the output format, by
-// the steps of store4 and store_nv_quad. NVFP4: lanes 2 j and 2 j + 1 hold the halves of
-// a 16-block and call this together.
-template <int OUT>
-__device__ __attribute__((always_inline)) inline void store8(const GemmArgs& g, int m, int n, const float (&y)[8], bool vec,
-                                                             float r, float st, float d) {
+// Bytes of `elements` (even) outputs.
+__device__ __attribute__((always_inline)) inline int64_t out_bytes(int out, int64_t elements) {
+  return out == OUT_F32 ? elements * 4 : out == OUT_FP8 ? elements : out == OUT_NVFP4 ? elements / 2 : elements * 2;
+}
+
+// Whether W consecutive outputs, from a multiple of W on, may be stored at once in
+// every row.
+template <int W>
+__device__ __attribute__((always_inline)) inline bool out_vec_of(const GemmArgs& g) {
+  const int64_t bytes = out_bytes(g.out_mode, W) < 16 ? out_bytes(g.out_mode, W) : 16;
+  return ((reinterpret_cast<uintptr_t>(g.y) & (bytes - 1)) == 0) && ((out_bytes(g.out_mode, g.ldy) & (bytes - 1)) == 0);
+}
+
+// W (4 or 8) consecutive outputs at o in the output format, by the steps of
+// store4 and store_nv_quad. NVFP4 (W = 8): lanes 2 j and 2 j + 1 hold the halves of a
+// 16-block and call this together; sb: its block scale's place.
+template <int OUT, int W>
+__device__ __attribute__((always_inline)) inline void store_run(uint8_t* o, uint8_t* sb, bool second, const float (&y)[W],
+                                                                bool vec, float r, float st, float d) {
   if constexpr (OUT == OUT_NVFP4) {
+    static_assert(W == 8, "half a block");
     uint32_t am = 0;
 #pragma unroll
     for (int j = 0; j < 8; ++j) am = max(am, f2u(y[j]) & 0x7FFFFFFFu);
     am = max(am, (uint32_t)__shfl_xor((int)am, 1));
     float rb;
-    const uint32_t sb = nv_block(am, st, d, rb);
+    const uint32_t code = nv_block(am, st, d, rb);
     float t[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) t[j] = __fmul_rn(y[j], rb);
-    uint8_t* row = reinterpret_cast<uint8_t*>(g.y) + (int64_t)m * (g.ldy >> 1);
-    *reinterpret_cast<uint32_t*>(row + (n >> 1)) = hw_e2m1x8(t);
-    if ((n & 15) == 0) g.y_bscale[(int64_t)m * (g.ldy >> 4) + (n >> 4)] = (uint8_t)sb;
-  } else if (!vec) {
-    store4(g, m, n, y[0], y[1], y[2], y[3], false, r);
-    store4(g, m, n + 4, y[4], y[5], y[6], y[7], false, r);
+    *reinterpret_cast<uint32_t*>(o) = hw_e2m1x8(t);
+    if (!second) *sb = (uint8_t)code;
   } else if constexpr (OUT == OUT_F32) {
-    float* o = reinterpret_cast<float*>(g.y) + (int64_t)m * g.ldy + n;
-    reinterpret_cast<float4*>(o)[0] = make_float4(y[0], y[1], y[2], y[3]);
-    reinterpret_cast<float4*>(o)[1] = make_float4(y[4], y[5], y[6], y[7]);
-  } else if constexpr (OUT == OUT_FP8) {
-    float t[8];
+    float* q = reinterpret_cast<float*>(o);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) t[j] = __fmul_rn(y[j], r);
-    *reinterpret_cast<uint2*>(reinterpret_cast<uint8_t*>(g.y) + (int64_t)m * g.ldy + n) =
-        make_uint2(hw_e4m3x4(t), hw_e4m3x4(t + 4));
+    for (int i = 0; i < W; i += 4) {
+      if (vec) *reinterpret_cast<float4*>(q + i) = make_float4(y[i], y[i + 1], y[i + 2], y[i + 3]);
+      else { q[i] = y[i]; q[i + 1] = y[i + 1]; q[i + 2] = y[i + 2]; q[i + 3] = y[i + 3]; }
+    }
+  } else if constexpr (OUT == OUT_FP8) {
+    float t[W];
+    uint32_t w[W / 4];
+#pragma unroll
+    for (int j = 0; j < W; ++j) t[j] = __fmul_rn(y[j], r);
+#pragma unroll
+    for (int j = 0; j < W / 4; ++j) w[j] = hw_e4m3x4(t + 4 * j);
+    if (!vec) {
+#pragma unroll
+      for (int j = 0; j < W; ++j) o[j] = (uint8_t)(w[j / 4] >> (8 * (j % 4)));
+    } else if constexpr (W == 8) {
+      *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+    } else {
+      *reinterpret_cast<uint32_t*>(o) = w[0];
+    }
   } else {
-    *reinterpret_cast<uint4*>(reinterpret_cast<uint16_t*>(g.y) + (int64_t)m * g.ldy + n) =
-        make_uint4(pk_bf16(y[0], y[1]), pk_bf16(y[2], y[3]), pk_bf16(y[4], y[5]), pk_bf16(y[6], y[7]));
+    uint32_t w[W / 2];
+#pragma unroll
+    for (int j = 0; j < W / 2; ++j) w[j] = pk_bf16(y[2 * j], y[2 * j + 1]);
+    if (!vec) {
+      uint16_t* q = reinterpret_cast<uint16_t*>(o);
+#pragma unroll
+      for (int j = 0; j < W; ++j) q[j] = (uint16_t)(w[j / 2] >> (16 * (j % 2)));
+    } else if constexpr (W == 8) {
+      *reinterpret_cast<uint4*>(o) = make_uint4(w[0], w[1], w[2], w[3]);
+    } else {
+      *reinterpret_cast<uint2*>(o) = make_uint2(w[0], w[1]);
+    }
   }
-}
-
-// Whether store8 may use aligned stores for every row of this output.
-__device__ __attribute__((always_inline)) inline bool out_vec8(const GemmArgs& g) {
-  const int bytes = g.out_mode == OUT_FP8 ? 8 : 16, esz = g.out_mode == OUT_F32 ? 4 : g.out_mode == OUT_FP8 ? 1 : 2;
-  return ((reinterpret_cast<uintptr_t>(g.y) & (bytes - 1)) == 0) && ((g.ldy * esz & (bytes - 1)) == 0);
 }
 
 // put(b) for the one of the constants K that b is. The empty statements differ in K: the
@@ -414,63 +444,113 @@ __device__ __attribute__((always_inline)) inline void put_block(int b, Put put, 
   (one(std::integral_constant<int, K>()), ...);
 }
 
-// The staged epilogue of a wave's sums, NB blocks of RB rows x CB columns, block b at
-// row m and column n of at(b, m, n): put(b) leaves a block in the wave's private LDS
-// area (row-major fp32, PITCH bytes a row) and every lane takes the columns of
-// eight outputs of a row, so that bias, residual and output are read and written in
-// whole row segments. Each wave reads back only what it wrote, so no barrier is needed.
-// The blocks are walked by a loop (only put is unrolled: accumulators have fixed
-// registers), the next block's residual under way while one is finished. In place
-// (residual the output) is fine: an element is read by the lane that writes it.
-template <int OUT, int NB, int RB, int CB, int PITCH, class Put, class At>
-__device__ __attribute__((always_inline)) inline void finish_blocks(const GemmArgs& g, const uint8_t* stage, int lane, float c,
-                                                                    Put put, At at) {
-  constexpr int Z = 8 * kPer, LPR = CB / Z, PIECES = RB * LPR, ITS = (PIECES + 63) / 64;
-  const bool vec = out_vec8(g);
+// How a wave takes its accumulators through its LDS area: blocks of sums in row-major
+// fp32, RB rows of CB columns (PITCH bytes a row), NI blocks down and NJ across; of a
+// block's ITS steps, step `it` gives a lane Z consecutive columns (W = Z / kPer outputs) of
+// row row0 + it STEP_ROWS from column col0 + it STEP_COLS on.
+struct Blocks32 {  // 32 x 32 MFMA tiles, two at a time
+  static constexpr int RB = 32, CB = 64, PITCH = CB * 4 + 16, Z = 8 * kPer, ITS = RB * CB / (64 * Z);
+  static constexpr int LPR = CB / Z, STEP_ROWS = 64 / LPR, STEP_COLS = 0, COLUMNS = 1;
+};
+struct Blocks16 {  // 16 x 16 MFMA tiles, the six of a wave's 96 columns at a time
+  static constexpr int RB = 16, CB = 96, PITCH = CB * 4 + 16, Z = 8, ITS = 3;
+  static constexpr int LPR = 4, STEP_ROWS = 0, STEP_COLS = 32, COLUMNS = 3;
+};
+
+// The staged epilogue of a wave's NI x NJ blocks of sums (first output row mw, weight
+// row nw): put(b) leaves block b = j NI + i in the LDS area, and every lane takes runs of
+// columns of a row, so that bias, residual and output are read and written in whole
+// row segments. Each wave reads back only what it wrote, so no barrier is needed. One
+// wave a SIMD runs here, so what counts is instructions: the blocks are walked by a
+// loop (only put is unrolled: accumulators have fixed registers) in one copy per
+// activation, with the addresses and the bias of a block column kept, and the next
+// block's residual under way while one is finished. In place (residual the output) is
+// fine: an element is read by the lane that writes it.
+template <class B, int OUT, int ACT, int NI, int NJ, class Put>
+__device__ __attribute__((always_inline)) inline void finish_blocks(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
+                                                                    int lane, float c, Put put) {
+  constexpr int Z = B::Z, W = Z / kPer, ITS = B::ITS;
+  const bool vec = out_vec_of<W>(g);
   const float r = OUT == OUT_FP8 ? out_rscale(g) : 0.0f;
   const float st = OUT == OUT_NVFP4 ? *g.y_scale : 0.0f, d = nv_out_d(g);
-  int row[ITS], col[ITS];
-#pragma unroll
-  for (int it = 0; it < ITS; ++it) {
-    const int idx = it * 64 + lane;
-    row[it] = (PIECES % 64 == 0 || idx < PIECES) ? idx / LPR : 1 << 30;  // (past every output)
-    col[it] = Z * (idx % LPR);
-  }
-  Run<8> next[ITS] = {}, res[ITS] = {};
+  const int row0 = lane / B::LPR, col0 = Z * (lane % B::LPR);
+  const uint8_t* rd = stage + row0 * B::PITCH + 4 * col0;
+  const int rows = g.m - mw - row0, cols = g.n - nw - col0;  // left from the lane's first on
+  const int64_t lane_out = out_bytes(OUT, (int64_t)row0 * g.ldy + col0 / kPer);
+  const int64_t lane_res = (int64_t)row0 * g.e.ldr + col0;
+  const bool residual = !kGated && g.e.residual != nullptr;
+  Run<W> next[ITS] = {}, res[ITS] = {};
+  float bias[B::COLUMNS][Z] = {};
   auto load = [&](int b) __attribute__((always_inline)) {
-    int m, n;
-    at(b, m, n);
+    const int i = B::RB * (b % NI), j = B::CB * (b / NI);
+    const int64_t at = (int64_t)(mw + i) * g.e.ldr + (nw + j);
 #pragma unroll
     for (int it = 0; it < ITS; ++it)
-      if (row[it] < g.m - m && n + col[it] < g.n) next[it] = load_residual<8>(g, m + row[it], n + col[it]);
+      if (i + it * B::STEP_ROWS < rows && j + it * B::STEP_COLS < cols)
+        next[it] = load_run<W>(g.e.residual, at + (int64_t)it * B::STEP_ROWS * g.e.ldr + it * B::STEP_COLS + lane_res,
+                               g.e.res_f32, g.e.res_vec);
   };
-  const bool residual = !kGated && g.e.residual != nullptr;
   if (residual) load(0);
 #pragma unroll 1
-  for (int b = 0; b < NB; ++b) {
+  for (int b = 0; b < NI * NJ; ++b) {
+    const int i = B::RB * (b % NI), j = B::CB * (b / NI);
     if (residual) {
 #pragma unroll
       for (int it = 0; it < ITS; ++it) res[it] = next[it];
-      if (b + 1 < NB) load(b + 1);
+      if (b + 1 < NI * NJ) load(b + 1);
     }
-    put_block(b, put, std::make_integer_sequence<int, NB>());
-    int m, n;
-    at(b, m, n);
+    if (g.e.bias && i == 0) {
+#pragma unroll
+      for (int k = 0; k < B::COLUMNS; ++k) {
+#pragma unroll
+        for (int v = 0; v < Z; ++v) bias[k][v] = 0.0f;
+        if (j + k * B::STEP_COLS < cols) {
+#pragma unroll
+          for (int h = 0; h < Z; h += 4)
+            add_run<4>(bias[k] + h, load_run<4>(g.e.bias, nw + j + k * B::STEP_COLS + col0 + h, g.e.bias_f32, g.e.bias_vec),
+                       g.e.bias_f32);
+        }
+      }
+    }
+    put_block(b, put, std::make_integer_sequence<int, NI * NJ>());
+    uint8_t* out = reinterpret_cast<uint8_t*>(g.y) + out_bytes(OUT, (int64_t)(mw + i) * g.ldy + (nw + j) / kPer) + lane_out;
+    uint8_t* sb = OUT == OUT_NVFP4
+        ? g.y_bscale + (int64_t)(mw + i + row0) * (g.ldy >> 4) + (((nw + j + col0) / kPer) >> 4) : nullptr;
 #pragma unroll
     for (int it = 0; it < ITS; ++it) {
-      const int mm = m + row[it], nn = n + col[it];
-      if (row[it] >= g.m - m || nn >= g.n) continue;
-      BiasRun<8> bias = {};
-      if (g.e.bias) bias = load_bias<8>(g, nn);
-      float z[Z], y[8];
+      if (i + it * B::STEP_ROWS >= rows || j + it * B::STEP_COLS >= cols) continue;
+      float z[Z], y[W];
 #pragma unroll
-      for (int i = 0; i < Z; i += 4) {
-        const float4 t = *reinterpret_cast<const float4*>(stage + row[it] * PITCH + 4 * (col[it] + i));
-        z[i] = t.x * c; z[i + 1] = t.y * c; z[i + 2] = t.z * c; z[i + 3] = t.w * c;
+      for (int v = 0; v < Z; v += 4) {
+        const float4 t = *reinterpret_cast<const float4*>(rd + it * (B::STEP_ROWS * B::PITCH + 4 * B::STEP_COLS) + 4 * v);
+        const float (&bz)[Z] = bias[B::COLUMNS == 1 ? 0 : it];
+        z[v] = __builtin_fmaf(t.x, c, bz[v]);
+        z[v + 1] = __builtin_fmaf(t.y, c, bz[v + 1]);
+        z[v + 2] = __builtin_fmaf(t.z, c, bz[v + 2]);
+        z[v + 3] = __builtin_fmaf(t.w, c, bz[v + 3]);
       }
-      finish<8>(g, bias, res[it], z, y);
-      store8<OUT>(g, mm, nn / kPer, y, vec, r, st, d);
+#pragma unroll
+      for (int v = 0; v < W; ++v) y[v] = activated<ACT>(z[kPer * v]);
+      if constexpr (kGated) {
+#pragma unroll
+        for (int v = 0; v < W; ++v) y[v] *= z[kPer * v + kPer - 1];
+      } else if (residual) {
+        add_run<W>(y, res[it], g.e.res_f32);
+      }
+      store_run<OUT, W>(out + out_bytes(OUT, (int64_t)it * B::STEP_ROWS * g.ldy + it * B::STEP_COLS / kPer),
+                        OUT == OUT_NVFP4 ? sb + it * B::STEP_ROWS * (g.ldy >> 4) : nullptr, lane & 1, y, vec, r, st, d);
     }
+  }
+}
+
+template <class B, int OUT, int NI, int NJ, class Put>
+__device__ __attribute__((always_inline)) inline void finish_all(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
+                                                                 int lane, float c, Put put) {
+  switch (g.e.act) {
+    case QG_ACT_SILU: finish_blocks<B, OUT, QG_ACT_SILU, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
+    case QG_ACT_GELU_TANH: finish_blocks<B, OUT, QG_ACT_GELU_TANH, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
+    case QG_ACT_GELU_ERF: finish_blocks<B, OUT, QG_ACT_GELU_ERF, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
+    default: finish_blocks<B, OUT, QG_ACT_NONE, NI, NJ>(g, stage, mw, nw, lane, c, put);
   }
 }
 #endif  // QG_EPILOGUE
@@ -574,26 +654,20 @@ __device__ __attribute__((always_inline)) inline void store_tiles(const GemmArgs
 #if QG_EPILOGUE
 // A wave's TM x TN accumulator tiles (layout as above) through its LDS area of kWaveStage
 // bytes, 32 rows of 64 columns at a time.
-constexpr int kWavePitch = 64 * 4 + 16, kWaveStage = 32 * kWavePitch;
+constexpr int kWaveStage = Blocks32::RB * Blocks32::PITCH;
 template <int OUT, int TM, int TN>
 __device__ __attribute__((always_inline)) inline void store_finished(const GemmArgs& g, const v16f (&acc)[TM][TN],
                                                                      uint8_t* stage, int mw, int nw, int lane, float c) {
-  constexpr int NJ = TN / 2;
-  uint8_t* wr = stage + (lane & 31) * kWavePitch + 16 * (lane >> 5);
-  auto put = [&](int b) __attribute__((always_inline)) {
+  uint8_t* wr = stage + (lane & 31) * Blocks32::PITCH + 16 * (lane >> 5);
+  finish_all<Blocks32, OUT, TM, TN / 2>(g, stage, mw, nw, lane, c, [&](int b) __attribute__((always_inline)) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int qd = 0; qd < 4; ++qd) {
-        const v16f& a = acc[b / NJ][b % NJ * 2 + j];
+        const v16f& a = acc[b % TM][b / TM * 2 + j];
         *reinterpret_cast<float4*>(wr + 128 * j + 32 * qd) = make_float4(a[4 * qd], a[4 * qd + 1], a[4 * qd + 2], a[4 * qd + 3]);
       }
-  };
-  auto at = [&](int b, int& m, int& n) __attribute__((always_inline)) {
-    m = mw + 32 * (b / NJ);
-    n = nw + 64 * (b % NJ);
-  };
-  finish_blocks<OUT, TM * NJ, 32, 64, kWavePitch>(g, stage, lane, c, put, at);
+  });
 }
 #endif
 
@@ -1208,7 +1282,7 @@ __global__ void __launch_bounds__(64 * NW) k_gemm_splitk(GemmArgs g) {
       }
       z[h] = sum.x * c; z[h + 1] = sum.y * c; z[h + 2] = sum.z * c; z[h + 3] = sum.w * c;
     }
-    finish_at<4>(g, m, n, z, y);
+    finish<4>(g, m, n, z, y);
     const int no = n / kPer;
     if (nv) store_nv_quad(g, m, no, y, st, d);
     else store4(g, m, no, y[0], y[1], y[2], y[3], vec, ry);
@@ -1794,23 +1868,17 @@ __device__ __attribute__((always_inline)) inline void store_t288(const GemmArgs&
 
 #if QG_EPILOGUE
 // The same for bias, activation, residual and gate: 16 rows of 96 columns of sums at a time.
-constexpr int kT288SumPitch = 96 * 4 + 16;
 template <int OUT>
 __device__ __attribute__((always_inline)) inline void store_t288_finished(const GemmArgs& g, const v4f (&acc)[9][6],
                                                                           uint8_t* stage, int mw, int nw, int lane, float c) {
-  uint8_t* wr = stage + (lane & 15) * kT288SumPitch + 16 * (lane >> 4);
-  auto put = [&](int b) __attribute__((always_inline)) {
+  uint8_t* wr = stage + (lane & 15) * Blocks16::PITCH + 16 * (lane >> 4);
+  finish_all<Blocks16, OUT, 9, 1>(g, stage, mw, nw, lane, c, [&](int b) __attribute__((always_inline)) {
 #pragma unroll
     for (int jj = 0; jj < 6; ++jj) {
       const v4f& a = acc[b][jj];
       *reinterpret_cast<float4*>(wr + 64 * jj) = make_float4(a[0], a[1], a[2], a[3]);
     }
-  };
-  auto at = [&](int b, int& m, int& n) __attribute__((always_inline)) {
-    m = mw + 16 * b;
-    n = nw;
-  };
-  finish_blocks<OUT, 9, 16, 96, kT288SumPitch>(g, stage, lane, c, put, at);
+  });
 }
 #endif
 
@@ -1820,7 +1888,7 @@ __global__ void __launch_bounds__(256) k_gemm_fp8_t288(GemmArgs g) {
   constexpr int RA = AStage288::RA;
   constexpr uint32_t OOB = 0x80000000u;
 #if QG_EPILOGUE
-  constexpr int OUT_STAGE = 16 * kT288SumPitch;
+  constexpr int OUT_STAGE = Blocks16::RB * Blocks16::PITCH;
 #else
   constexpr int OUT_STAGE = 16 * kT288Pitch;    // output staging: 16 rows of 96 bf16 + pad
 #endif
@@ -3158,7 +3226,7 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
         }
         z[4 * h] = sum.x * c; z[4 * h + 1] = sum.y * c; z[4 * h + 2] = sum.z * c; z[4 * h + 3] = sum.w * c;
       }
-      finish_at<4>(g, m, n, z, y);
+      finish<4>(g, m, n, z, y);
       store4(g, m, n >> 1, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
     }
     continue;
@@ -3176,7 +3244,7 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
       if (m >= g.m || n >= g.n) continue;
 #if QG_EPILOGUE == 1
       float z[4] = {sum.x * c, sum.y * c, sum.z * c, sum.w * c}, y[4];
-      finish_at<4>(g, m, n, z, y);
+      finish<4>(g, m, n, z, y);
       store4(g, m, n, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
 #else
       store4(g, m, n, sum.x * c, sum.y * c, sum.z * c, sum.w * c, out_vec(g), out_rscale(g));
@@ -3457,7 +3525,7 @@ __global__ void __launch_bounds__(256) k_finish_rows(GemmArgs g) {
     float y[16];
     for (int h = 0; h < 16; h += 4) {
       float z[4 * kPer] = {}, y4[4];
-      finish_at<4>(g, m, (n + h) * kPer, z, y4);
+      finish<4>(g, m, (n + h) * kPer, z, y4);
       for (int i = 0; i < 4; ++i) y[h + i] = y4[i];
     }
     if (g.out_mode != OUT_NVFP4) {
