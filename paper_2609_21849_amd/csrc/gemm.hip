@@ -216,44 +216,65 @@ __device__ __attribute__((always_inline)) inline void store_nv_quad(const GemmAr
 //              term, least in its largest relative error (2e-8; fitted by reweighted
 //              least squares over x / sqrt 2 in [0, 9.5]); no cancellation at z < 0
 // Far negative z: the exponential is inf, its reciprocal 0, the result -0.
-__device__ __attribute__((always_inline)) inline float logistic(float t) {
-  return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(t * -1.44269504f));
-}
 
-__device__ __attribute__((always_inline)) inline float normal_cdf(float z) {
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.21213203f, __builtin_fabsf(z), 1.0f));
-  float p = -0.06471703946590424f;
-  p = __builtin_fmaf(p, t, 0.24254822731018066f);
-  p = __builtin_fmaf(p, t, -0.2556132376194f);
-  p = __builtin_fmaf(p, t, 0.2731975317001343f);
-  p = __builtin_fmaf(p, t, -0.046815626323223114f);
-  p = __builtin_fmaf(p, t, 0.10721813887357712f);
-  p = __builtin_fmaf(p, t, 0.07424121350049973f);
-  p = __builtin_fmaf(p, t, 0.08534596860408783f);
-  p = __builtin_fmaf(p, t, 0.08459480851888657f);
-  const float tail = t * p * __builtin_amdgcn_exp2f(z * z * -0.72134752f);
-  return z < 0.0f ? tail : 1.0f - tail;
-}
-
-template <int ACT>
-__device__ __attribute__((always_inline)) inline float activated(float z) {
-  if constexpr (ACT == QG_ACT_SILU) return z * logistic(z);
-  else if constexpr (ACT == QG_ACT_GELU_TANH) return z * logistic(1.59576912f * z * __builtin_fmaf(0.044715f * z, z, 1.0f));
-  else if constexpr (ACT == QG_ACT_GELU_ERF) return z * normal_cdf(z);
-  else return z;
-}
-
-template <int W>
-__device__ __attribute__((always_inline)) inline void activate(float (&v)[W], int act) {
-  if (act == QG_ACT_SILU) {
+// The values in registers here, all at once: what makes them is not moved past this
+// point, so that independent chains run beside each other instead of one after the
+// other in the same few registers (one wave a SIMD: nothing else hides their latency).
+template <int N>
+__device__ __attribute__((always_inline)) inline void together(float (&v)[N]) {
+  if constexpr (N % 4 != 0) {
+    static_assert(N == 1, "whole groups, or nothing to order");
+  } else if constexpr (N % 8 == 0) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_SILU>(v[i]);
-  } else if (act == QG_ACT_GELU_TANH) {
+    for (int i = 0; i < N; i += 8)
+      asm volatile("" : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3]), "+v"(v[i + 4]), "+v"(v[i + 5]),
+                   "+v"(v[i + 6]), "+v"(v[i + 7]));
+  } else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_GELU_TANH>(v[i]);
+    for (int i = 0; i < N; i += 4) asm volatile("" : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3]));
+  }
+}
+
+// v = act(v), step by step for all values.
+template <int N>
+__device__ __attribute__((always_inline)) inline void activate(float (&v)[N], int act) {
+  float t[N];
+  if (act == QG_ACT_SILU || act == QG_ACT_GELU_TANH) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = v[i];
+    if (act == QG_ACT_GELU_TANH) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) t[i] = 1.59576912f * v[i] * __builtin_fmaf(0.044715f * v[i], v[i], 1.0f);
+      together(t);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_exp2f(t[i] * -1.44269504f);
+    together(t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_rcpf(1.0f + t[i]);
+    together(t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= t[i];
   } else if (act == QG_ACT_GELU_ERF) {
+    float p[N];
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] = activated<QG_ACT_GELU_ERF>(v[i]);
+    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_rcpf(__builtin_fmaf(0.21213203f, __builtin_fabsf(v[i]), 1.0f));
+    together(t);
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = __builtin_fmaf(-0.06471703946590424f, t[i], 0.24254822731018066f);
+    constexpr float kP[7] = {-0.2556132376194f,    0.2731975317001343f,  -0.046815626323223114f, 0.10721813887357712f,
+                             0.07424121350049973f, 0.08534596860408783f, 0.08459480851888657f};
+#pragma unroll
+    for (int k = 0; k < 7; ++k) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) p[i] = __builtin_fmaf(p[i], t[i], kP[k]);
+      together(p);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] *= t[i] * __builtin_amdgcn_exp2f(v[i] * v[i] * -0.72134752f);
+    together(p);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= v[i] < 0.0f ? p[i] : 1.0f - p[i];
   }
 }
 
@@ -296,15 +317,15 @@ __device__ __attribute__((always_inline)) inline Run<W> load_run(const void* p, 
   return t;
 }
 template <int W>
-__device__ __attribute__((always_inline)) inline void add_run(float* v, const Run<W>& t, bool f32) {
+__device__ __attribute__((always_inline)) inline void values(const Run<W>& t, bool f32, float* v) {
   if (f32) {
 #pragma unroll
-    for (int i = 0; i < W; ++i) v[i] += u2f(t.w[i]);
+    for (int i = 0; i < W; ++i) v[i] = u2f(t.w[i]);
   } else {
 #pragma unroll
     for (int i = 0; i < W / 2; ++i) {
-      v[2 * i] += bf16_lo(t.w[i]);
-      v[2 * i + 1] += bf16_hi(t.w[i]);
+      v[2 * i] = bf16_lo(t.w[i]);
+      v[2 * i + 1] = bf16_hi(t.w[i]);
     }
   }
 }
@@ -312,21 +333,24 @@ __device__ __attribute__((always_inline)) inline void add_run(float* v, const Ru
 // Weight rows, so accumulator columns, of one output.
 constexpr int kPer = kGated ? 2 : 1;
 
-// W outputs m, n / kPer on from the scaled sums z of kPer W consecutive weight rows
-// from n on, with their bias and residual.
+// W outputs m, n / kPer on from the sums of kPer W consecutive weight rows from n on
+// (c: their scale), with their bias and residual. z = fl(sum c + bias) in every
+// kernel, so that equal sums give equal outputs.
 template <int W>
-__device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, int m, int n, float (&z)[kPer * W],
-                                                             float (&y)[W]) {
-  Run<W> b[kPer], res;
+__device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, int m, int n, float c,
+                                                             const float (&sum)[kPer * W], float (&y)[W]) {
+  float z[kPer * W], res[W];
+#pragma unroll
+  for (int h = 0; h < kPer * W; ++h) z[h] = 0.0f;
+  if (!kGated && g.e.residual)
+    values<W>(load_run<W>(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32, g.e.res_vec), g.e.res_f32, res);
   if (g.e.bias) {
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) b[h] = load_run<W>(g.e.bias, n + h * W, g.e.bias_f32, g.e.bias_vec);
+    for (int h = 0; h < kPer; ++h)
+      values<W>(load_run<W>(g.e.bias, n + h * W, g.e.bias_f32, g.e.bias_vec), g.e.bias_f32, z + h * W);
   }
-  if (!kGated && g.e.residual) res = load_run<W>(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32, g.e.res_vec);
-  if (g.e.bias) {
 #pragma unroll
-    for (int h = 0; h < kPer; ++h) add_run<W>(z + h * W, b[h], g.e.bias_f32);
-  }
+  for (int i = 0; i < kPer * W; ++i) z[i] = __builtin_fmaf(sum[i], c, z[i]);
 #pragma unroll
   for (int i = 0; i < W; ++i) y[i] = z[kPer * i];
   activate(y, g.e.act);
@@ -334,18 +358,19 @@ __device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, 
 #pragma unroll
     for (int i = 0; i < W; ++i) y[i] *= z[kPer * i + kPer - 1];
   } else if (g.e.residual) {
-    add_run<W>(y, res, g.e.res_f32);
+#pragma unroll
+    for (int i = 0; i < W; ++i) y[i] += res[i];
   }
 }
 
-// One output from the scaled sum of one column held by each lane (the weight-pool
+// One output from the sum of one column held by each lane (the weight-pool
 // kernels); false where the lane holds an up projection, whose gate's lane (one
 // lower) has the output.
-__device__ __attribute__((always_inline)) inline bool finish1(const GemmArgs& g, int m, int& n, float& z) {
+__device__ __attribute__((always_inline)) inline bool finish1(const GemmArgs& g, int m, int& n, float c, float& z) {
   auto at = [](const void* p, int64_t i, bool f32) {
     return f32 ? reinterpret_cast<const float*>(p)[i] : u2f((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
   };
-  if (g.e.bias) z += at(g.e.bias, n, g.e.bias_f32);
+  z = __builtin_fmaf(z, c, g.e.bias ? at(g.e.bias, n, g.e.bias_f32) : 0.0f);
   const float up = kGated ? __shfl_xor(z, 1) : 0.0f;
   float y[1] = {z};
   activate(y, g.e.act);
@@ -444,6 +469,10 @@ __device__ __attribute__((always_inline)) inline void put_block(int b, Put put, 
   (one(std::integral_constant<int, K>()), ...);
 }
 
+// Longest row pitch (elements) of finish_wide: a wave's tile of up to 144 rows of fp32
+// stays below 2^31 bytes.
+constexpr int64_t kWidePitch = int64_t(1) << 21;
+
 // How a wave takes its accumulators through its LDS area: blocks of sums in row-major
 // fp32, RB rows of CB columns (PITCH bytes a row), NI blocks down and NJ across; of a
 // block's ITS steps, step `it` gives a lane Z consecutive columns (W = Z / kPer outputs) of
@@ -460,85 +489,189 @@ struct Blocks16 {  // 16 x 16 MFMA tiles, the six of a wave's 96 columns at a ti
 // The staged epilogue of a wave's NI x NJ blocks of sums (first output row mw, weight
 // row nw): put(b) leaves block b = j NI + i in the LDS area, and every lane takes runs of
 // columns of a row, so that bias, residual and output are read and written in whole
-// row segments. Each wave reads back only what it wrote, so no barrier is needed. One
-// wave a SIMD runs here, so what counts is instructions: the blocks are walked by a
-// loop (only put is unrolled: accumulators have fixed registers) in one copy per
-// activation, with the addresses and the bias of a block column kept, and the next
-// block's residual under way while one is finished. In place (residual the output) is
-// fine: an element is read by the lane that writes it.
-template <class B, int OUT, int ACT, int NI, int NJ, class Put>
-__device__ __attribute__((always_inline)) inline void finish_blocks(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
-                                                                    int lane, float c, Put put) {
-  constexpr int Z = B::Z, W = Z / kPer, ITS = B::ITS;
-  const bool vec = out_vec_of<W>(g);
+// row segments. Each wave reads back only what it wrote, so no barrier is needed. The
+// blocks are walked by a loop (only put is unrolled: accumulators have fixed registers).
+// In place (residual the output) is fine: an element is read by the lane that writes it.
+//
+// finish_wide, where every run may be loaded and stored at once (g.e.wide): one wave a
+// SIMD runs here, so what costs is instructions and waits. Straight-line code between
+// the uniform branches, rows and columns past the output masked by out-of-range buffer
+// offsets; a block's residual is loaded while the block before it is stored (RES: 0
+// none, 1 bf16, 2 fp32).
+template <class B, int OUT, int RES, int NI, int NJ, class Put>
+__device__ __attribute__((always_inline)) inline void finish_wide(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
+                                                                  int lane, float c, Put put) {
+  constexpr int Z = B::Z, W = Z / kPer, ITS = B::ITS, COLUMNS = B::COLUMNS;
+  constexpr uint32_t OOB = 0x80000000u;
   const float r = OUT == OUT_FP8 ? out_rscale(g) : 0.0f;
   const float st = OUT == OUT_NVFP4 ? *g.y_scale : 0.0f, d = nv_out_d(g);
   const int row0 = lane / B::LPR, col0 = Z * (lane % B::LPR);
   const uint8_t* rd = stage + row0 * B::PITCH + 4 * col0;
   const int rows = g.m - mw - row0, cols = g.n - nw - col0;  // left from the lane's first on
-  const int64_t lane_out = out_bytes(OUT, (int64_t)row0 * g.ldy + col0 / kPer);
-  const int64_t lane_res = (int64_t)row0 * g.e.ldr + col0;
-  const bool residual = !kGated && g.e.residual != nullptr;
-  Run<W> next[ITS] = {}, res[ITS] = {};
-  float bias[B::COLUMNS][Z] = {};
-  auto load = [&](int b) __attribute__((always_inline)) {
-    const int i = B::RB * (b % NI), j = B::CB * (b / NI);
-    const int64_t at = (int64_t)(mw + i) * g.e.ldr + (nw + j);
+  // outputs of a wave's tile: below 2^31 bytes from its first on (pitches of at most kWidePitch)
+  const __amdgpu_buffer_rsrc_t rs_y = __builtin_amdgcn_make_buffer_rsrc(
+      reinterpret_cast<uint8_t*>(g.y) + out_bytes(OUT, (int64_t)mw * g.ldy + nw / kPer), 0, 0x7FFFFFFF, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rs_s = __builtin_amdgcn_make_buffer_rsrc(
+      g.y_bscale + (int64_t)mw * (g.ldy >> 4) + (nw / kPer >> 4), 0, 0x7FFFFFFF, 0x00020000);
+  constexpr int RSZ = RES == 2 ? 4 : 2;
+  const __amdgpu_buffer_rsrc_t rs_r = __builtin_amdgcn_make_buffer_rsrc(
+      const_cast<uint8_t*>(reinterpret_cast<const uint8_t*>(g.e.residual)) + ((int64_t)mw * g.e.ldr + nw) * RSZ, 0,
+      0x7FFFFFFF, 0x00020000);
+  const int ldy = (int)g.ldy, ldr = (int)g.e.ldr;
+  auto bytes = [](int elements) { return (int)out_bytes(OUT, elements); };
+  const int out0 = bytes(row0 * ldy + col0 / kPer), res0 = (row0 * ldr + col0) * RSZ, sb0 = row0 * (ldy >> 4) + (col0 / kPer >> 4);
+
+  float bias[NJ * COLUMNS][Z];
 #pragma unroll
-    for (int it = 0; it < ITS; ++it)
-      if (i + it * B::STEP_ROWS < rows && j + it * B::STEP_COLS < cols)
-        next[it] = load_run<W>(g.e.residual, at + (int64_t)it * B::STEP_ROWS * g.e.ldr + it * B::STEP_COLS + lane_res,
-                               g.e.res_f32, g.e.res_vec);
-  };
-  if (residual) load(0);
-#pragma unroll 1
-  for (int b = 0; b < NI * NJ; ++b) {
-    const int i = B::RB * (b % NI), j = B::CB * (b / NI);
-    if (residual) {
+  for (int k = 0; k < NJ * COLUMNS; ++k)
 #pragma unroll
-      for (int it = 0; it < ITS; ++it) res[it] = next[it];
-      if (b + 1 < NI * NJ) load(b + 1);
+    for (int v = 0; v < Z; ++v) bias[k][v] = 0.0f;
+  if (g.e.bias) {
+#pragma unroll
+    for (int k = 0; k < NJ * COLUMNS; ++k) {
+      const int at = COLUMNS == 1 ? k * B::CB : k * B::STEP_COLS;
+      if (at < cols) {
+#pragma unroll
+        for (int h = 0; h < Z; h += 4)
+          values<4>(load_run<4>(g.e.bias, nw + at + col0 + h, g.e.bias_f32, true), g.e.bias_f32, bias[k] + h);
+      }
+      together(bias[k]);
     }
-    if (g.e.bias && i == 0) {
+  }
+  uint32_t res[ITS][RES == 2 ? W : W / 2];
+  auto inside = [&](int i, int j, int it) __attribute__((always_inline)) {
+    return i + it * B::STEP_ROWS < rows && j + it * B::STEP_COLS < cols;
+  };
+  auto load = [&](int b) __attribute__((always_inline)) {
+    const int i = B::RB * (b % NI), j = B::CB * (b / NI), so = (i * ldr + j) * RSZ;
 #pragma unroll
-      for (int k = 0; k < B::COLUMNS; ++k) {
+    for (int it = 0; it < ITS; ++it) {
+      const uint32_t off = inside(i, j, it) ? (uint32_t)(res0 + (it * B::STEP_ROWS * ldr + it * B::STEP_COLS) * RSZ) : OOB;
+      if constexpr (W * RSZ == 8) {
+        const v2i t = __builtin_amdgcn_raw_buffer_load_b64(rs_r, off, so, 0);
+        res[it][0] = (uint32_t)t.x;
+        res[it][1] = (uint32_t)t.y;
+      } else {
 #pragma unroll
-        for (int v = 0; v < Z; ++v) bias[k][v] = 0.0f;
-        if (j + k * B::STEP_COLS < cols) {
-#pragma unroll
-          for (int h = 0; h < Z; h += 4)
-            add_run<4>(bias[k] + h, load_run<4>(g.e.bias, nw + j + k * B::STEP_COLS + col0 + h, g.e.bias_f32, g.e.bias_vec),
-                       g.e.bias_f32);
+        for (int h = 0; h < W * RSZ / 16; ++h) {
+          const v4i t = __builtin_amdgcn_raw_buffer_load_b128(rs_r, off + 16 * h, so, 0);
+          res[it][4 * h] = (uint32_t)t.x;
+          res[it][4 * h + 1] = (uint32_t)t.y;
+          res[it][4 * h + 2] = (uint32_t)t.z;
+          res[it][4 * h + 3] = (uint32_t)t.w;
         }
       }
     }
-    put_block(b, put, std::make_integer_sequence<int, NI * NJ>());
-    uint8_t* out = reinterpret_cast<uint8_t*>(g.y) + out_bytes(OUT, (int64_t)(mw + i) * g.ldy + (nw + j) / kPer) + lane_out;
-    uint8_t* sb = OUT == OUT_NVFP4
-        ? g.y_bscale + (int64_t)(mw + i + row0) * (g.ldy >> 4) + (((nw + j + col0) / kPer) >> 4) : nullptr;
+  };
+  if constexpr (RES != 0) load(0);
+#pragma unroll 1
+  for (int b = 0; b < NI * NJ; ++b) {
+    const int i = B::RB * (b % NI), j = B::CB * (b / NI);
+    if (NJ > 1 && b == NI) {  // the second block column's bias
 #pragma unroll
-    for (int it = 0; it < ITS; ++it) {
-      if (i + it * B::STEP_ROWS >= rows || j + it * B::STEP_COLS >= cols) continue;
-      float z[Z], y[W];
+      for (int v = 0; v < Z; ++v) bias[0][v] = bias[NJ - 1][v];
+    }
+    put_block(b, put, std::make_integer_sequence<int, NI * NJ>());
+    float z[ITS][Z], y[ITS * W];
+#pragma unroll
+    for (int it = 0; it < ITS; ++it)
 #pragma unroll
       for (int v = 0; v < Z; v += 4) {
         const float4 t = *reinterpret_cast<const float4*>(rd + it * (B::STEP_ROWS * B::PITCH + 4 * B::STEP_COLS) + 4 * v);
-        const float (&bz)[Z] = bias[B::COLUMNS == 1 ? 0 : it];
-        z[v] = __builtin_fmaf(t.x, c, bz[v]);
-        z[v + 1] = __builtin_fmaf(t.y, c, bz[v + 1]);
-        z[v + 2] = __builtin_fmaf(t.z, c, bz[v + 2]);
-        z[v + 3] = __builtin_fmaf(t.w, c, bz[v + 3]);
+        const float (&bz)[Z] = bias[COLUMNS == 1 ? 0 : it];
+        z[it][v] = __builtin_fmaf(t.x, c, bz[v]);
+        z[it][v + 1] = __builtin_fmaf(t.y, c, bz[v + 1]);
+        z[it][v + 2] = __builtin_fmaf(t.z, c, bz[v + 2]);
+        z[it][v + 3] = __builtin_fmaf(t.w, c, bz[v + 3]);
       }
 #pragma unroll
-      for (int v = 0; v < W; ++v) y[v] = activated<ACT>(z[kPer * v]);
-      if constexpr (kGated) {
+    for (int it = 0; it < ITS; ++it)
 #pragma unroll
-        for (int v = 0; v < W; ++v) y[v] *= z[kPer * v + kPer - 1];
-      } else if (residual) {
-        add_run<W>(y, res[it], g.e.res_f32);
+      for (int v = 0; v < W; ++v) y[it * W + v] = z[it][kPer * v];
+    activate(y, g.e.act);
+    if constexpr (kGated) {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it)
+#pragma unroll
+        for (int v = 0; v < W; ++v) y[it * W + v] *= z[it][kPer * v + kPer - 1];
+    }
+    if constexpr (RES != 0) {
+#pragma unroll
+      for (int it = 0; it < ITS; ++it)
+#pragma unroll
+        for (int v = 0; v < W; ++v)
+          y[it * W + v] += RES == 2 ? u2f(res[it][v]) : v % 2 ? bf16_hi(res[it][v / 2]) : bf16_lo(res[it][v / 2]);
+      together(y);
+      load(min(b + 1, NI * NJ - 1));
+    }
+    const int so = bytes(i * ldy + j / kPer);
+#pragma unroll
+    for (int it = 0; it < ITS; ++it) {
+      const float* v = y + it * W;
+      const bool in = inside(i, j, it);
+      const uint32_t off = in ? (uint32_t)(out0 + bytes(it * B::STEP_ROWS * ldy + it * B::STEP_COLS / kPer)) : OOB;
+      if constexpr (OUT == OUT_NVFP4) {
+        uint32_t am = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) am = max(am, f2u(v[e]) & 0x7FFFFFFFu);
+        am = max(am, (uint32_t)__shfl_xor((int)am, 1));
+        float rb, t[8];
+        const uint32_t sb = nv_block(am, st, d, rb);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) t[e] = __fmul_rn(v[e], rb);
+        __builtin_amdgcn_raw_buffer_store_b32((int)hw_e2m1x8(t), rs_y, off, so, 0);
+        __builtin_amdgcn_raw_buffer_store_b8((char)sb, rs_s, in && !(lane & 1) ? (uint32_t)(sb0 + it * B::STEP_ROWS * (ldy >> 4)) : OOB,
+                                             i * (ldy >> 4) + (j / kPer >> 4), 0);
+      } else if constexpr (OUT == OUT_F32) {
+#pragma unroll
+        for (int h = 0; h < W; h += 4)
+          __builtin_amdgcn_raw_buffer_store_b128((v4i){(int)f2u(v[h]), (int)f2u(v[h + 1]), (int)f2u(v[h + 2]), (int)f2u(v[h + 3])},
+                                                 rs_y, off + 4 * h, so, 0);
+      } else if constexpr (OUT == OUT_FP8) {
+        float t[W];
+#pragma unroll
+        for (int e = 0; e < W; ++e) t[e] = __fmul_rn(v[e], r);
+        if constexpr (W == 8)
+          __builtin_amdgcn_raw_buffer_store_b64((v2i){(int)hw_e4m3x4(t), (int)hw_e4m3x4(t + 4)}, rs_y, off, so, 0);
+        else
+          __builtin_amdgcn_raw_buffer_store_b32((int)hw_e4m3x4(t), rs_y, off, so, 0);
+      } else if constexpr (W == 8) {
+        __builtin_amdgcn_raw_buffer_store_b128((v4i){(int)pk_bf16(v[0], v[1]), (int)pk_bf16(v[2], v[3]), (int)pk_bf16(v[4], v[5]),
+                                                     (int)pk_bf16(v[6], v[7])}, rs_y, off, so, 0);
+      } else {
+        __builtin_amdgcn_raw_buffer_store_b64((v2i){(int)pk_bf16(v[0], v[1]), (int)pk_bf16(v[2], v[3])}, rs_y, off, so, 0);
       }
-      store_run<OUT, W>(out + out_bytes(OUT, (int64_t)it * B::STEP_ROWS * g.ldy + it * B::STEP_COLS / kPer),
-                        OUT == OUT_NVFP4 ? sb + it * B::STEP_ROWS * (g.ldy >> 4) : nullptr, lane & 1, y, vec, r, st, d);
+    }
+  }
+}
+
+// The same for outputs, residuals and biases of any alignment and pitch.
+template <class B, int OUT, int NI, int NJ, class Put>
+__device__ __attribute__((always_inline)) inline void finish_any(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
+                                                                 int lane, float c, Put put) {
+  constexpr int Z = B::Z, W = Z / kPer;
+  const bool vec = out_vec_of<W>(g);
+  const float r = OUT == OUT_FP8 ? out_rscale(g) : 0.0f;
+  const float st = OUT == OUT_NVFP4 ? *g.y_scale : 0.0f, d = nv_out_d(g);
+  const int row0 = lane / B::LPR, col0 = Z * (lane % B::LPR);
+#pragma unroll 1
+  for (int b = 0; b < NI * NJ; ++b) {
+    put_block(b, put, std::make_integer_sequence<int, NI * NJ>());
+#pragma unroll 1
+    for (int it = 0; it < B::ITS; ++it) {
+      const int row = row0 + it * B::STEP_ROWS, col = col0 + it * B::STEP_COLS;
+      const int m = mw + B::RB * (b % NI) + row, n = nw + B::CB * (b / NI) + col;
+      if (m >= g.m || n >= g.n) continue;
+      float z[Z], y[W];
+#pragma unroll
+      for (int v = 0; v < Z; v += 4) {
+        const float4 t = *reinterpret_cast<const float4*>(stage + row * B::PITCH + 4 * (col + v));
+        z[v] = t.x; z[v + 1] = t.y; z[v + 2] = t.z; z[v + 3] = t.w;
+      }
+      finish<W>(g, m, n, c, z, y);
+      store_run<OUT, W>(reinterpret_cast<uint8_t*>(g.y) + out_bytes(OUT, (int64_t)m * g.ldy + n / kPer),
+                        OUT == OUT_NVFP4 ? g.y_bscale + (int64_t)m * (g.ldy >> 4) + (n / kPer >> 4) : nullptr, lane & 1, y, vec,
+                        r, st, d);
     }
   }
 }
@@ -546,12 +679,20 @@ __device__ __attribute__((always_inline)) inline void finish_blocks(const GemmAr
 template <class B, int OUT, int NI, int NJ, class Put>
 __device__ __attribute__((always_inline)) inline void finish_all(const GemmArgs& g, const uint8_t* stage, int mw, int nw,
                                                                  int lane, float c, Put put) {
-  switch (g.e.act) {
-    case QG_ACT_SILU: finish_blocks<B, OUT, QG_ACT_SILU, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
-    case QG_ACT_GELU_TANH: finish_blocks<B, OUT, QG_ACT_GELU_TANH, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
-    case QG_ACT_GELU_ERF: finish_blocks<B, OUT, QG_ACT_GELU_ERF, NI, NJ>(g, stage, mw, nw, lane, c, put); break;
-    default: finish_blocks<B, OUT, QG_ACT_NONE, NI, NJ>(g, stage, mw, nw, lane, c, put);
+  mw = __builtin_amdgcn_readfirstlane(mw);
+  nw = __builtin_amdgcn_readfirstlane(nw);
+  if (!g.e.wide) {
+    finish_any<B, OUT, NI, NJ>(g, stage, mw, nw, lane, c, put);
+    return;
   }
+  if constexpr (!kGated) {
+    if (g.e.residual) {
+      if (g.e.res_f32) finish_wide<B, OUT, 2, NI, NJ>(g, stage, mw, nw, lane, c, put);
+      else finish_wide<B, OUT, 1, NI, NJ>(g, stage, mw, nw, lane, c, put);
+      return;
+    }
+  }
+  finish_wide<B, OUT, 0, NI, NJ>(g, stage, mw, nw, lane, c, put);
 }
 #endif  // QG_EPILOGUE
 
@@ -1280,9 +1421,9 @@ __global__ void __launch_bounds__(64 * NW) k_gemm_splitk(GemmArgs g) {
         const float4 v = *reinterpret_cast<const float4*>(p + w * (BM * LDR));
         sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
       }
-      z[h] = sum.x * c; z[h + 1] = sum.y * c; z[h + 2] = sum.z * c; z[h + 3] = sum.w * c;
+      z[h] = sum.x; z[h + 1] = sum.y; z[h + 2] = sum.z; z[h + 3] = sum.w;
     }
-    finish<4>(g, m, n, z, y);
+    finish<4>(g, m, n, c, z, y);
     const int no = n / kPer;
     if (nv) store_nv_quad(g, m, no, y, st, d);
     else store4(g, m, no, y[0], y[1], y[2], y[3], vec, ry);
@@ -3224,9 +3365,9 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
           const float4 v = *reinterpret_cast<const float4*>(p + w * MT * 1024);
           sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
         }
-        z[4 * h] = sum.x * c; z[4 * h + 1] = sum.y * c; z[4 * h + 2] = sum.z * c; z[4 * h + 3] = sum.w * c;
+        z[4 * h] = sum.x; z[4 * h + 1] = sum.y; z[4 * h + 2] = sum.z; z[4 * h + 3] = sum.w;
       }
-      finish<4>(g, m, n, z, y);
+      finish<4>(g, m, n, c, z, y);
       store4(g, m, n >> 1, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
     }
     continue;
@@ -3243,8 +3384,9 @@ __global__ void __launch_bounds__(64 * NW) k_w4a16_splitk(GemmArgs g) {
       const int n = (panel * NP + j) * 32 + 8 * q + 4 * (l >> 5);
       if (m >= g.m || n >= g.n) continue;
 #if QG_EPILOGUE == 1
-      float z[4] = {sum.x * c, sum.y * c, sum.z * c, sum.w * c}, y[4];
-      finish<4>(g, m, n, z, y);
+      const float z[4] = {sum.x, sum.y, sum.z, sum.w};
+      float y[4];
+      finish<4>(g, m, n, c, z, y);
       store4(g, m, n, y[0], y[1], y[2], y[3], out_vec(g), out_rscale(g));
 #else
       store4(g, m, n, sum.x * c, sum.y * c, sum.z * c, sum.w * c, out_vec(g), out_rscale(g));
@@ -3380,8 +3522,8 @@ __global__ void __launch_bounds__(64 * NWV) k_w4a16_stream(GemmArgs g) {
           const int m = 8 * (v >> 2) + 4 * gq + (v & 3);
           if (m >= g.m) continue;
           int n = nz;
-          float y = acc[v] * c;
-          if (!finish1(g, m, n, y)) continue;
+          float y = acc[v];
+          if (!finish1(g, m, n, c, y)) continue;
 #else
       const int n = panel * 32 + r;
       if (n < g.n) {
@@ -3496,10 +3638,10 @@ __global__ void __launch_bounds__(512, 4) k_w4a16_gemv(GemmArgs g) {
     if (nk == 0) {
       // panel done: row r's two halves sit in lanes r and r + 32
 #if QG_EPILOGUE
-      float v = (acc + __shfl_xor(acc, 32)) * c;
+      float v = acc + __shfl_xor(acc, 32);
       acc = 0.0f;
       int n = panel * 32 + r;
-      if (gq == 0 && n < g.n && finish1(g, 0, n, v)) {
+      if (gq == 0 && n < g.n && finish1(g, 0, n, c, v)) {
 #else
       const float v = (acc + __shfl_xor(acc, 32)) * c;
       acc = 0.0f;
@@ -3525,7 +3667,7 @@ __global__ void __launch_bounds__(256) k_finish_rows(GemmArgs g) {
     float y[16];
     for (int h = 0; h < 16; h += 4) {
       float z[4 * kPer] = {}, y4[4];
-      finish<4>(g, m, (n + h) * kPer, z, y4);
+      finish<4>(g, m, (n + h) * kPer, 1.0f, z, y4);
       for (int i = 0; i < 4; ++i) y[h + i] = y4[i];
     }
     if (g.out_mode != OUT_NVFP4) {
@@ -3756,6 +3898,10 @@ hipError_t launch(int a_fmt, const void* a, const uint8_t* a_bscale, const float
   // eight elements in one load (fp32 two): a row's pieces start at multiples of eight
   g.e.bias_vec = reinterpret_cast<uintptr_t>(e.bias) % 16 == 0;
   g.e.res_vec = reinterpret_cast<uintptr_t>(e.residual) % 16 == 0 && e.ldr * (e.res_f32 ? 4 : 2) % 16 == 0;
+  const int64_t unit = out_mode == OUT_FP8 ? 8 : out_mode == OUT_NVFP4 ? 4 : 16, pitch = ldy * (out_mode == OUT_F32 ? 4 : 2);
+  g.e.wide = reinterpret_cast<uintptr_t>(y) % unit == 0 &&
+             (out_mode == OUT_NVFP4 || (out_mode == OUT_FP8 ? ldy : pitch) % unit == 0) && ldy <= kWidePitch &&
+             (!e.bias || g.e.bias_vec) && (!e.residual || (g.e.res_vec && e.ldr <= kWidePitch));
   if (k > 0) return launch_product(a_fmt, g, st);
   const int64_t groups = (m * (n / 16) + 255) / 256;
   hipLaunchKernelGGL(k_finish_rows, dim3((unsigned)std::min<int64_t>(groups, 65536)), dim3(256), 0, st, g);

@@ -52,13 +52,14 @@ hipError_t launch_gemm(int a_fmt, const void* a, const uint8_t* a_bscale, const 
                        void* y, int64_t ldy, int out_mode, const float* y_scale, uint8_t* y_bscale,
                        hipStream_t st);
 // What qg_gemm_fused does with the sums: bias [n], activation (qg_activation),
-// residual [m, ldr]; bf16 or fp32. The *_vec are the launcher's: aligned for wide loads.
+// residual [m, ldr]; bf16 or fp32. The launcher's: *_vec, aligned for wide loads; wide,
+// those and the output.
 struct Epilogue {
   const void* bias;
   const void* residual;
   int64_t ldr;
   int act;
-  bool bias_f32, bias_vec, res_f32, res_vec;
+  bool bias_f32, bias_vec, res_f32, res_vec, wide;
 };
 // launch_gemm with that epilogue (out_mode as there). gated: rows 2 i and 2 i + 1 of
 // the [n, k] weight are output i's gate and up rows; y has n / 2 columns, no residual.
