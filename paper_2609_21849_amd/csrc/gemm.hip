@@ -240,15 +240,16 @@ template <int N>
 __device__ __attribute__((always_inline)) inline void activate(float (&v)[N], int act) {
   float t[N];
   if (act == QG_ACT_SILU || act == QG_ACT_GELU_TANH) {
+    // -log2 e times the logistic function's argument; GELU: -2 sqrt(2 / pi) log2 e (1 + 0.044715 z^2) z
 #pragma unroll
-    for (int i = 0; i < N; ++i) t[i] = v[i];
+    for (int i = 0; i < N; ++i) t[i] = v[i] * -1.44269504f;
     if (act == QG_ACT_GELU_TANH) {
 #pragma unroll
-      for (int i = 0; i < N; ++i) t[i] = 1.59576912f * v[i] * __builtin_fmaf(0.044715f * v[i], v[i], 1.0f);
-      together(t);
+      for (int i = 0; i < N; ++i) t[i] = v[i] * __builtin_fmaf(v[i] * v[i], -0.102943240f, -2.30220820f);
     }
+    together(t);
 #pragma unroll
-    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_exp2f(t[i] * -1.44269504f);
+    for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_exp2f(t[i]);
     together(t);
 #pragma unroll
     for (int i = 0; i < N; ++i) t[i] = __builtin_amdgcn_rcpf(1.0f + t[i]);

@@ -90,7 +90,11 @@ struct NormArgs {
   int64_t ldy;
   uint8_t* bscale;
   float* tscale;        // FP8, NVFP4: read (static) or written
-  uint32_t* partial;    // the launcher's
+  // the launcher's, for a tensor scale taken from y
+  uint32_t* partial;    // maxima of the first launch's workgroups, or (regions > 0)
+  int64_t regions;      // one of each in so many regions of y,
+  int64_t region_bytes; // so far apart,
+  int slots;            // so many in each
 };
 hipError_t launch_rms_norm(int fmt, const NormArgs& a, bool static_scale, hipStream_t st);
 // W8A8 linear from bf16 activations x [m, ldx] (16-byte aligned rows):

@@ -17,10 +17,13 @@
 //
 // A tensor scale taken from y (dynamic FP8, NVFP4) needs the largest |y| of all
 // rows before the first code: one workgroup does a tensor of few rows in one launch;
-// otherwise the first launch writes h and a maximum per workgroup (parked in the
-// code buffer that the last one overwrites), the second makes the scale of them, the
-// third norms h again, with the same steps, and codes it.
+// otherwise a first launch writes h and a maximum per workgroup, parked in the code
+// buffer, and the last one norms h again, with the same steps, and codes it. Between
+// them k_norm_scale makes the scale of the maxima; or, for tensors of moderate size, the
+// first launch leaves its maxima at the start of every workgroup's own codes, where
+// the last finds them (launch_dynamic).
 #include <algorithm>
+#include <type_traits>
 
 #include "common.hpp"
 #include "kernels.hpp"
@@ -162,20 +165,12 @@ __device__ __attribute__((always_inline)) inline void store_y(const NormArgs& a,
 }
 
 // ---------------------------------------------------------------- reductions
-__device__ __attribute__((always_inline)) inline float wave_sum(float v) {
-  for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off);
-  return v;
-}
-__device__ __attribute__((always_inline)) inline uint32_t wave_max(uint32_t v) {
-  for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
-  return v;
-}
-
-// Over the TPR threads of a row, the whole workgroup if more than a wave; red: words
-// that no thread still reads.
+// Over the TPR threads of a row: part of a wave, a wave, or the whole workgroup; red:
+// words that no thread still reads.
 template <int TPR>
 __device__ __attribute__((always_inline)) inline float row_sum(float v, float* red) {
-  v = wave_sum(v);
+#pragma unroll
+  for (int off = (TPR < 64 ? TPR : 64) / 2; off > 0; off >>= 1) v += __shfl_xor(v, off);
   if constexpr (TPR > 64) {
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -183,6 +178,10 @@ __device__ __attribute__((always_inline)) inline float row_sum(float v, float* r
 #pragma unroll
     for (int i = 1; i < TPR / 64; ++i) v += red[i];
   }
+  return v;
+}
+__device__ __attribute__((always_inline)) inline uint32_t wave_max(uint32_t v) {
+  for (int off = 32; off > 0; off >>= 1) v = max(v, (uint32_t)__shfl_xor((int)v, off));
   return v;
 }
 
@@ -211,16 +210,74 @@ __device__ __attribute__((always_inline)) inline float scale_of_max(uint32_t m, 
 }
 
 // ---------------------------------------------------------------- rows in registers
-// TPR threads share a row, NV units of 16 elements each: unit t + TPR i. TPR = 64: a
-// workgroup has a row per wave at a time, else one row. DYN: the workgroup holds every
-// row of the tensor, so its largest |y| gives the tensor scale, which it writes.
-template <int FMT, int NV, int TPR, bool DYN>
-__global__ void __launch_bounds__(DYN || TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs a) {
+// TPR threads share a row, NV units of 16 elements each: unit t + TPR i. TPR <= 64: a
+// workgroup has blockDim / TPR rows at a time, else one. One or two units a thread
+// measured best at nearly every size (12 shapes from 1 x 1024 to 16384 x 4096, TPR 64 to
+// 1024, units of 8 and 16): static FP8 with a residual 4608 x 3072 22.7 us (4.4 TB/s)
+// with a workgroup per row against 25.3 with a wave, 500 x 3072 5.3 against 6.7, 16384 x
+// 4096 84.7 (5.5 TB/s) against 91.1.
+//
+// Row `row` of thread t: h, and what its elements are multiplied by before the weight.
+template <int NV, int TPR>
+__device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a, int64_t row, int t, float (&red)[2][16],
+                                                               int& turn, uint32_t (&h)[NV][8], float& pre, float& rstd) {
+  float ss = 0.0f;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = 16 * (t + TPR * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) h[i][j] = 0u;
+    if (c < a.cols) load_h(a, row, c, a.cols - c, h[i]);
+  }
+#pragma unroll
+  for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, 1.0f);
+  ss = row_sum<TPR>(ss, red[turn]);
+  turn ^= 1;
+  pre = 1.0f;
+  rstd = rstd_of(ss, a.cols, a.eps);
+  if (!(ss <= 3.40282347e38f)) {  // the same in every thread of the row
+    pre = kHugeScale;
+    ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, pre);
+    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, 0.0f);
+    turn ^= 1;
+  }
+}
+
+// fn(first column, elements left in the row, the 16 values of y) for the thread's units.
+template <int NV, int TPR, class F>
+__device__ __attribute__((always_inline)) inline void each_unit(const NormArgs& a, int t, const uint32_t (&h)[NV][8], float pre,
+                                                                float rstd, F fn) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i) {
+    const int c = 16 * (t + TPR * i);
+    if (c >= a.cols) continue;
+    float w[16], y[16];
+    load_weight(a, c, a.cols - c, w);
+    norm16(h[i], w, pre, rstd, y);
+    fn(c, a.cols - c, y);
+  }
+}
+
+// The largest |y| of a workgroup's rows, to where the launch that codes them reads it:
+// one word a workgroup, or (a.regions) one in each of that launch's workgroups' codes.
+__device__ __attribute__((always_inline)) inline void leave_max(const NormArgs& a, uint32_t am) {
+  am = group_max(am);
+  if (a.regions == 0) {
+    if (threadIdx.x == 0) a.partial[blockIdx.x] = am;
+    return;
+  }
+  for (int64_t j = threadIdx.x; j < a.regions; j += blockDim.x)
+    reinterpret_cast<uint32_t*>(a.y + j * a.region_bytes)[blockIdx.x] = am;
+}
+
+template <int FMT, int NV, int TPR>
+__global__ void __launch_bounds__(TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs a) {
   __shared__ float red[2][16];
   const int t = (int)threadIdx.x % TPR, rpb = (int)blockDim.x / TPR;
-  const float divisor = FMT == F_FP8 ? 448.0f : 2688.0f;
   float s = 0.0f, r = 0.0f;
-  if ((FMT == F_FP8 || FMT == F_NVFP4) && !DYN) {
+  if (FMT == F_FP8 || FMT == F_NVFP4) {
     s = *a.tscale;
     r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
   }
@@ -228,59 +285,45 @@ __global__ void __launch_bounds__(DYN || TPR == 1024 ? 1024 : 256) k_rms_norm(No
   int turn = 0;
   for (int64_t row = (int64_t)blockIdx.x * rpb + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * rpb) {
     uint32_t h[NV][8];
-    float ss = 0.0f;
-#pragma unroll
-    for (int i = 0; i < NV; ++i) {
-      const int c = 16 * (t + TPR * i);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) h[i][j] = 0u;
-      if (c < a.cols) load_h(a, row, c, a.cols - c, h[i]);
-    }
-#pragma unroll
-    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, 1.0f);
-    ss = row_sum<TPR>(ss, red[turn]);
-    turn ^= 1;
-    float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
-    if (!(ss <= 3.40282347e38f)) {  // the same in every thread of the row
-      pre = kHugeScale;
-      ss = 0.0f;
-#pragma unroll
-      for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, pre);
-      rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, 0.0f);
-      turn ^= 1;
-    }
-    if constexpr (FMT == F_AMAX || DYN) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = 16 * (t + TPR * i);
-        if (c >= a.cols) continue;
-        float w[16], y[16];
-        load_weight(a, c, a.cols - c, w);
-        norm16(h[i], w, pre, rstd, y);
-        am = max(am, amax16(y));
-      }
-    }
-    if constexpr (DYN) {  // one turn of the loop: every row of the tensor is here
-      s = scale_of_max(group_max(am), divisor);
-      r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
-      if (threadIdx.x == 0) *a.tscale = s;
-    }
-    if constexpr (FMT != F_AMAX) {
-#pragma unroll
-      for (int i = 0; i < NV; ++i) {
-        const int c = 16 * (t + TPR * i);
-        if (c >= a.cols) continue;
-        float w[16], y[16];
-        load_weight(a, c, a.cols - c, w);
-        norm16(h[i], w, pre, rstd, y);
-        store_y<FMT>(a, row, c, a.cols - c, y, s, r);
-      }
-    }
+    float pre, rstd;
+    norm_row<NV, TPR>(a, row, t, red, turn, h, pre, rstd);
+    each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
+      if constexpr (FMT == F_AMAX) am = max(am, amax16(y));
+      else store_y<FMT>(a, row, c, cnt, y, s, r);
+    });
   }
-  if constexpr (FMT == F_AMAX) {
-    am = group_max(am);
-    if (threadIdx.x == 0) a.partial[blockIdx.x] = am;
+  if constexpr (FMT == F_AMAX) leave_max(a, am);
+}
+
+// FP8 and NVFP4 with the tensor scale taken from y, where every workgroup has its rows in
+// one turn. SLOTS: from the maxima that the launch before left at the start of this
+// workgroup's codes (all read before the barrier that any code is written after);
+// otherwise the only workgroup's own, which holds every row of the tensor.
+template <int FMT, int NV, int TPR, bool SLOTS>
+__global__ void __launch_bounds__(SLOTS && TPR < 1024 ? 256 : 1024) k_rms_norm_scaled(NormArgs a) {
+  __shared__ float red[2][16];
+  const int t = (int)threadIdx.x % TPR, rpb = (int)blockDim.x / TPR;
+  const int64_t row = (int64_t)blockIdx.x * rpb + threadIdx.x / TPR;
+  const bool live = row < a.rows;  // (one row a workgroup: always)
+  uint32_t h[NV][8], am = 0;
+  float pre = 1.0f, rstd = 0.0f;
+  int turn = 0;
+  if (live) norm_row<NV, TPR>(a, row, t, red, turn, h, pre, rstd);
+  if constexpr (SLOTS) {
+    const uint32_t* slots = reinterpret_cast<const uint32_t*>(a.y + (int64_t)blockIdx.x * a.region_bytes);
+    for (int i = (int)threadIdx.x; i < a.slots; i += (int)blockDim.x) am = max(am, slots[i]);
+  } else if (live) {
+    each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int, int, const float (&y)[16]) __attribute__((always_inline)) {
+      am = max(am, amax16(y));
+    });
   }
+  const float s = scale_of_max(group_max(am), FMT == F_FP8 ? 448.0f : 2688.0f);
+  const float r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
+  if (blockIdx.x == 0 && threadIdx.x == 0) *a.tscale = s;
+  if (!live) return;
+  each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
+    store_y<FMT>(a, row, c, cnt, y, s, r);
+  });
 }
 
 // Rows too long for the registers: a workgroup walks the row twice (three times
@@ -332,10 +375,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
       else store_y<FMT>(a, row, (int)c, cnt, y, s, r);
     }
   }
-  if constexpr (FMT == F_AMAX) {
-    am = group_max(am);
-    if (threadIdx.x == 0) a.partial[blockIdx.x] = am;
-  }
+  if constexpr (FMT == F_AMAX) leave_max(a, am);
 }
 
 // The tensor scale from `count` maxima (fp32 bits), which may lie in `scale` itself.
@@ -349,68 +389,119 @@ __global__ void __launch_bounds__(256) k_norm_scale(const uint32_t* partial, int
 __global__ void k_norm_empty(float* scale) { *scale = 0.0f; }
 
 // ---------------------------------------------------------------- launchers
-constexpr int64_t kNormGroups = 2048;  // eight workgroups of 256 threads a CU
+// Workgroups of a launch (each thread count stays below 2^32), and of one that leaves a
+// maximum each for k_norm_scale.
+constexpr int64_t kNormGroups = int64_t(1) << 20, kNormMaxGroups = 2048;
 
-// Threads that share a row of `units` 16-element units (0: too long for registers).
-static int threads_per_row(int64_t units) {
-  return units <= 64 * 4 ? 64 : units <= 256 * 4 ? 256 : units <= 1024 * 4 ? 1024 : 0;
+// Up to one row a CU of more than 256 units takes as many threads as a workgroup has.
+constexpr int64_t kNormFewRows = 256;
+
+struct NormPlan {
+  int tpr, nv;     // threads that share a row (0: too long for the registers) and their units
+  int64_t rpb;     // rows of a workgroup
+  int64_t groups;  // workgroups that have every row in one turn
+};
+static NormPlan norm_plan(int64_t rows, int64_t cols) {
+  const int64_t units = (cols + 15) / 16;
+  NormPlan p;
+  p.tpr = 0;
+  if (units <= 128) {
+    for (p.tpr = 8; p.tpr < units; p.tpr *= 2) {}
+  } else if (units <= 256 || (units <= 256 * 4 && rows > kNormFewRows)) {
+    p.tpr = 256;
+  } else if (units <= 1024 * 3) {
+    p.tpr = 1024;
+  }
+  p.nv = p.tpr ? (int)((units + p.tpr - 1) / p.tpr) : 0;
+  p.rpb = p.tpr != 0 && p.tpr <= 64 ? 256 / p.tpr : 1;
+  p.groups = (rows + p.rpb - 1) / p.rpb;
+  return p;
 }
 
-template <int FMT, bool DYN>
-static void launch_rows(const NormArgs& a, int tpr, unsigned groups, unsigned threads, hipStream_t st) {
-  const int64_t units = ((int64_t)a.cols + 15) / 16;
-  const int nv = tpr ? (int)((units + tpr - 1) / tpr) : 0;
-#define QG_NORM(NV, TPR) hipLaunchKernelGGL((k_rms_norm<FMT, NV, TPR, DYN>), dim3(groups), dim3(threads), 0, st, a)
-#define QG_NORM_NV(TPR)                                                                            \
-  do {                                                                                             \
-    if (nv == 1) QG_NORM(1, TPR);                                                                  \
-    else if (nv == 2) QG_NORM(2, TPR);                                                             \
-    else if (nv == 3) QG_NORM(3, TPR);                                                             \
-    else QG_NORM(4, TPR);                                                                          \
-  } while (0)
-  if (tpr == 64) QG_NORM_NV(64);
-  else if (tpr == 256) QG_NORM_NV(256);
-  else if (tpr == 1024) QG_NORM_NV(1024);
-  else if constexpr (!DYN) hipLaunchKernelGGL((k_rms_norm_long<FMT>), dim3(groups), dim3(1024), 0, st, a);
-#undef QG_NORM_NV
-#undef QG_NORM
+// fn(NV, TPR) as constants.
+template <class F>
+static void with_plan(const NormPlan& p, F fn) {
+  const auto call = [&]<int NV, int TPR>() { fn(std::integral_constant<int, NV>(), std::integral_constant<int, TPR>()); };
+  switch (p.tpr) {
+    case 8: call.template operator()<1, 8>(); break;
+    case 16: call.template operator()<1, 16>(); break;
+    case 32: call.template operator()<1, 32>(); break;
+    case 64: call.template operator()<1, 64>(); break;
+    case 128: call.template operator()<1, 128>(); break;
+    case 256:
+      if (p.nv == 1) call.template operator()<1, 256>();
+      else if (p.nv == 2) call.template operator()<2, 256>();
+      else if (p.nv == 3) call.template operator()<3, 256>();
+      else call.template operator()<4, 256>();
+      break;
+    default:
+      if (p.nv == 1) call.template operator()<1, 1024>();
+      else if (p.nv == 2) call.template operator()<2, 1024>();
+      else call.template operator()<3, 1024>();
+  }
 }
 
 template <int FMT>
-static void launch_all(const NormArgs& a, int64_t groups_max, hipStream_t st) {
-  const int tpr = threads_per_row(((int64_t)a.cols + 15) / 16);
-  const int64_t rpb = tpr == 64 ? 4 : 1;
-  const unsigned groups = (unsigned)std::min<int64_t>((a.rows + rpb - 1) / rpb, groups_max);
-  launch_rows<FMT, false>(a, tpr, groups, tpr == 64 ? 256 : tpr ? tpr : 1024, st);
+static void launch_all(const NormArgs& a, const NormPlan& p, int64_t groups_max, hipStream_t st) {
+  const unsigned groups = (unsigned)std::min(p.groups, groups_max);
+  if (p.tpr == 0) {
+    hipLaunchKernelGGL((k_rms_norm_long<FMT>), dim3(groups), dim3(1024), 0, st, a);
+    return;
+  }
+  with_plan(p, [&](auto NV, auto TPR) {
+    hipLaunchKernelGGL((k_rms_norm<FMT, NV(), TPR()>), dim3(groups), dim3((unsigned)(p.rpb * p.tpr)), 0, st, a);
+  });
 }
+
+template <int FMT, bool SLOTS>
+static void launch_scaled(const NormArgs& a, const NormPlan& p, unsigned groups, unsigned threads, hipStream_t st) {
+  with_plan(p, [&](auto NV, auto TPR) {
+    hipLaunchKernelGGL((k_rms_norm_scaled<FMT, NV(), TPR(), SLOTS>), dim3(groups), dim3(threads), 0, st, a);
+  });
+}
+
+// Up to so many workgroups the maxima are left in every workgroup's codes: a launch
+// less for groups^2 scattered words (dynamic FP8 with a residual 300 x 1024, 75 groups,
+// 8.4 us in three launches, 7.2 in two; 128 x 3072, 128, 8.5, 7.6; 1024 x 1024, 256, 9.6, 8.8;
+// 300 x 9216, 300, 14.7, 14.0; 500 x 3072, 500, 11.0, 12.1).
+constexpr int64_t kNormSlots = 256;
 
 // A tensor scale taken from y.
 template <int FMT>
 static hipError_t launch_dynamic(NormArgs a, hipStream_t st) {
-  const int tpr = threads_per_row(((int64_t)a.cols + 15) / 16);
-  if ((tpr == 64 && a.rows <= 16) || (tpr != 0 && a.rows == 1)) {
-    launch_rows<FMT, true>(a, tpr, 1, (unsigned)(a.rows * tpr), st);
+  const NormPlan p = norm_plan(a.rows, a.cols);
+  if (p.tpr != 0 && (p.tpr <= 64 ? a.rows * p.tpr <= 1024 : a.rows == 1)) {
+    launch_scaled<FMT, false>(a, p, 1, (unsigned)((a.rows * p.tpr + 63) / 64 * 64), st);
     return hipGetLastError();
   }
-  const int64_t bytes = FMT == F_FP8 ? a.rows * a.cols : a.rows * a.cols / 2;
+  const int64_t row_bytes = FMT == F_FP8 ? (int64_t)a.cols : (int64_t)a.cols / 2;
+  NormArgs b = a;  // the last launch: reads the stored sum where there is one
+  if (a.res && a.sum) {
+    b.x = a.sum;
+    b.ldx = a.lds;
+    b.res = nullptr;
+  }
+  b.sum = nullptr;
+  if (p.tpr != 0 && p.groups <= std::min(kNormSlots, row_bytes / 4) && row_bytes % 4 == 0 &&
+      reinterpret_cast<uintptr_t>(a.y) % 4 == 0) {
+    a.regions = p.groups;
+    a.region_bytes = b.region_bytes = p.rpb * row_bytes;
+    b.slots = (int)p.groups;
+    launch_all<F_AMAX>(a, p, p.groups, st);
+    launch_scaled<FMT, true>(b, p, (unsigned)p.groups, (unsigned)(p.rpb * p.tpr), st);
+    return hipGetLastError();
+  }
   const uintptr_t base = (reinterpret_cast<uintptr_t>(a.y) + 3) & ~uintptr_t(3);
-  const int64_t cap = (bytes - (int64_t)(base - reinterpret_cast<uintptr_t>(a.y))) / 4;
-  const int64_t rpb = tpr == 64 ? 4 : 1;
-  int64_t groups = std::min<int64_t>((a.rows + rpb - 1) / rpb, kNormGroups);
+  const int64_t cap = (a.rows * row_bytes - (int64_t)(base - reinterpret_cast<uintptr_t>(a.y))) / 4;
+  int64_t groups = std::min(p.groups, kNormMaxGroups);
   a.partial = reinterpret_cast<uint32_t*>(base);
   if (groups > cap) {  // short rows: one workgroup, its maximum straight into the scale's place
     groups = 1;
     a.partial = reinterpret_cast<uint32_t*>(a.tscale);
   }
-  launch_all<F_AMAX>(a, groups, st);
+  launch_all<F_AMAX>(a, p, groups, st);
   hipLaunchKernelGGL(k_norm_scale, dim3(1), dim3(256), 0, st, a.partial, (int)groups, a.tscale, FMT == F_FP8 ? 448.0f : 2688.0f);
-  if (a.res && a.sum) {
-    a.x = a.sum;
-    a.ldx = a.lds;
-    a.res = nullptr;
-  }
-  a.sum = nullptr;
-  launch_all<FMT>(a, kNormGroups, st);
+  launch_all<FMT>(b, p, kNormGroups, st);
   return hipGetLastError();
 }
 
@@ -422,11 +513,12 @@ hipError_t launch_rms_norm(int fmt, const NormArgs& a, bool static_scale, hipStr
   }
   if (fmt == F_FP8 && !static_scale) return launch_dynamic<F_FP8>(a, st);
   if (fmt == F_NVFP4 && !static_scale) return launch_dynamic<F_NVFP4>(a, st);
-  if (fmt == F_FP8) launch_all<F_FP8>(a, kNormGroups, st);
-  else if (fmt == F_NVFP4) launch_all<F_NVFP4>(a, kNormGroups, st);
-  else if (fmt == F_MXFP4) launch_all<F_MXFP4>(a, kNormGroups, st);
-  else if (fmt == F_MXFP8) launch_all<F_MXFP8>(a, kNormGroups, st);
-  else launch_all<F_BF16>(a, kNormGroups, st);
+  const NormPlan p = norm_plan(a.rows, a.cols);
+  if (fmt == F_FP8) launch_all<F_FP8>(a, p, kNormGroups, st);
+  else if (fmt == F_NVFP4) launch_all<F_NVFP4>(a, p, kNormGroups, st);
+  else if (fmt == F_MXFP4) launch_all<F_MXFP4>(a, p, kNormGroups, st);
+  else if (fmt == F_MXFP8) launch_all<F_MXFP8>(a, p, kNormGroups, st);
+  else launch_all<F_BF16>(a, p, kNormGroups, st);
   return hipGetLastError();
 }
 

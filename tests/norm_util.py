@@ -1,8 +1,9 @@
 """What qg_rms_norm may return, from its formula in 64 bits.
 
-y = fl(fl(h r) w) in fp32. With u = 2^-24 and L the longest chain of fp32
-additions behind the sum of squares (16 elements of each of a thread's units,
-six lane swaps, the waves), all terms positive: the sum is within (L + 1) u of
+y = fl(fl(h r) w) in fp32. With u = 2^-24 and L at least the longest chain of
+fp32 additions behind the sum of squares (16 elements of each of a thread's
+units, at most four of them up to 16384 columns and ceil(cols / 16384) past
+that, six lane swaps, the waves), all terms positive: the sum is within (L + 1) u of
 the exact one relatively, the mean one division, eps one addition, so the root
 of it within half of (L + 3) u plus one rounding; the reciprocal and the two
 products round once each: |y - y64| <= ((L + 3) / 2 + 4) u |y64|. A quantized
@@ -20,7 +21,7 @@ U = 2.0 ** -24
 
 def rel_error(cols: int) -> float:
     units = -(-cols // 16)
-    per_thread = -(-units // 64) if units <= 256 else -(-units // 256) if units <= 1024 else -(-units // 1024)
+    per_thread = max(4, -(-units // 1024))
     return ((16 * per_thread + 6 + 16 + 3) / 2 + 4) * U
 
 

@@ -40,7 +40,11 @@ def _check(x, w, residual, fmt, static=False, eps=EPS, **kw):
 # one wave a row (1 to 4 units a lane), a workgroup a row (256 and 1024 threads), rows past the registers; one token,
 # a few (one launch with the tensor's scale), many; row ends inside a unit
 SHAPES = [(1, 32), (1, 1024), (16, 1024), (17, 1024), (3, 2080), (300, 1024), (9, 3072), (5, 4096), (1, 4128), (4, 5120),
-          (37, 9216), (1, 16384), (2, 16416), (3, 65536), (2, 65568), (1, 131104)]
+          (37, 9216), (1, 16384), (2, 16416), (3, 65536), (2, 65568), (1, 131104),
+          # several rows a wave (one launch, maxima in every workgroup's codes, three launches); a thread's units by the
+          # number of rows; the longest rows in registers
+          (100, 128), (1000, 128), (9000, 96), (70, 224), (300, 512), (129, 480), (2100, 480), (257, 6144), (256, 6144),
+          (300, 1600), (60, 20000), (3, 49152), (2, 49184)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
