@@ -364,26 +364,35 @@ __device__ __attribute__((always_inline)) inline void finish(const GemmArgs& g, 
   }
 }
 
-// One output from the sum of one column held by each lane (the weight-pool
-// kernels); false where the lane holds an up projection, whose gate's lane (one
-// lower) has the output.
-__device__ __attribute__((always_inline)) inline bool finish1(const GemmArgs& g, int m, int& n, float c, float& z) {
+// The weight-pool kernels: a lane's sums of weight row n, one for each of MV output rows
+// (row(v); those from g.m on are not stored). kGated: the lane of the gate, one below
+// that of the up projection, has the output.
+template <int MV, class Row>
+__device__ __attribute__((always_inline)) inline void finish_column(const GemmArgs& g, int n, float c, float (&z)[MV], Row row) {
   auto at = [](const void* p, int64_t i, bool f32) {
     return f32 ? reinterpret_cast<const float*>(p)[i] : u2f((uint32_t)reinterpret_cast<const uint16_t*>(p)[i] << 16);
   };
-  z = __builtin_fmaf(z, c, g.e.bias ? at(g.e.bias, n, g.e.bias_f32) : 0.0f);
-  const float up = kGated ? __shfl_xor(z, 1) : 0.0f;
-  float y[1] = {z};
-  activate(y, g.e.act);
-  if (kGated) {
-    z = y[0] * up;
-    const bool gate = (n & 1) == 0;
-    n >>= 1;
-    return gate;
+  const float bias = g.e.bias ? at(g.e.bias, n, g.e.bias_f32) : 0.0f;
+  float up[MV];
+#pragma unroll
+  for (int v = 0; v < MV; ++v) z[v] = __builtin_fmaf(z[v], c, bias);
+  if constexpr (kGated) {
+#pragma unroll
+    for (int v = 0; v < MV; ++v) up[v] = __shfl_xor(z[v], 1);
   }
-  z = y[0];
-  if (g.e.residual) z += at(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32);
-  return true;
+  activate(z, g.e.act);
+  if (kGated && (n & 1)) return;
+  n /= kPer;
+#pragma unroll
+  for (int v = 0; v < MV; ++v) {
+    const int m = row(v);
+    if (m >= g.m) continue;
+    float y = z[v];
+    if constexpr (kGated) y *= up[v];
+    else if (g.e.residual) y += at(g.e.residual, (int64_t)m * g.e.ldr + n, g.e.res_f32);
+    if (g.out_mode == OUT_F32) reinterpret_cast<float*>(g.y)[(int64_t)m * g.ldy + n] = y;
+    else reinterpret_cast<uint16_t*>(g.y)[(int64_t)m * g.ldy + n] = (uint16_t)pk_bf16(y, 0.0f);
+  }
 }
 
 // Bytes of `elements` (even) outputs.
@@ -3534,29 +3543,21 @@ __global__ void __launch_bounds__(64 * NWV) k_w4a16_stream(GemmArgs g) {
     compute(cb, kc0);
     if (nk == 0) {
       // panel done: lane (r, g) holds column n = 32 panel + r of rows 8 (v / 4) + 4 g + v % 4
-#if QG_EPILOGUE
-      const int nz = panel * 32 + r;
-      if (nz < g.n) {
-#pragma unroll
-        for (int v = 0; v < MV; ++v) {
-          const int m = 8 * (v >> 2) + 4 * gq + (v & 3);
-          if (m >= g.m) continue;
-          int n = nz;
-          float y = acc[v];
-          if (!finish1(g, m, n, c, y)) continue;
-#else
       const int n = panel * 32 + r;
+#if QG_EPILOGUE
+      if (n < g.n) finish_column(g, n, c, acc, [&](int v) { return 8 * (v >> 2) + 4 * gq + (v & 3); });
+#else
       if (n < g.n) {
 #pragma unroll
         for (int v = 0; v < MV; ++v) {
           const int m = 8 * (v >> 2) + 4 * gq + (v & 3);
           if (m >= g.m) continue;
           const float y = acc[v] * c;
-#endif
           if (g.out_mode == OUT_F32) reinterpret_cast<float*>(g.y)[(int64_t)m * g.ldy + n] = y;
           else reinterpret_cast<uint16_t*>(g.y)[(int64_t)m * g.ldy + n] = (uint16_t)pk_bf16(y, 0.0f);
         }
       }
+#endif
     }
     panel = np_;
     kc0 = nk;
@@ -3658,19 +3659,19 @@ __global__ void __launch_bounds__(512, 4) k_w4a16_gemv(GemmArgs g) {
     if (nk == 0) {
       // panel done: row r's two halves sit in lanes r and r + 32
 #if QG_EPILOGUE
-      float v = acc + __shfl_xor(acc, 32);
+      float v[1] = {acc + __shfl_xor(acc, 32)};
       acc = 0.0f;
-      int n = panel * 32 + r;
-      if (gq == 0 && n < g.n && finish1(g, 0, n, c, v)) {
+      const int n = panel * 32 + r;
+      if (gq == 0 && n < g.n) finish_column(g, n, c, v, [](int) { return 0; });
 #else
       const float v = (acc + __shfl_xor(acc, 32)) * c;
       acc = 0.0f;
       const int n = panel * 32 + r;
       if (gq == 0 && n < g.n) {
-#endif
         if (g.out_mode == OUT_F32) reinterpret_cast<float*>(g.y)[n] = v;
         else reinterpret_cast<uint16_t*>(g.y)[n] = (uint16_t)pk_bf16(v, 0.0f);
       }
+#endif
     }
     panel = np_;
     kc0 = nk;
