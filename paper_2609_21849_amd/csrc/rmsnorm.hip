@@ -33,21 +33,44 @@ namespace qg {
 enum { F_BF16 = 0, F_FP8 = 1, F_NVFP4 = 2, F_MXFP4 = 3, F_MXFP8 = 4, F_AMAX = 5 };  // qg_format; F_AMAX: h and max |y| alone
 
 // ---------------------------------------------------------------- 16 elements of a row
-// cnt (from the unit's first to the row's last element) >= 16: whole.
-__device__ __attribute__((always_inline)) inline void load16(const uint16_t* p, int cnt, uint32_t (&w)[8]) {
-  if (cnt >= 16) {
-    __builtin_memcpy(w, p, 32);
+// Elements [c, c + 16) of a row of cols, zero from cols on. EVEN: cols % 16 == 0, every
+// unit whole (an instance of its own: with the code for shorter units behind branches
+// the others take 10 % longer, 4608 x 3072 23.4 us, now 20.6). A row's last unit, if shorter, is loaded as the row's last 16 elements and shifted down, the same in every row: one
+// latency, where a condition on each element made 16 loads follow each other (a row of
+// fewer than 16 elements still takes them).
+template <int N>  // words; down by `words` of them
+__device__ __attribute__((always_inline)) inline void shift_down(uint32_t (&w)[N], int words) {
+#pragma unroll
+  for (int k = N / 2; k > 0; k >>= 1)
+    if (words & k) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) w[i] = i + k < N ? w[i + k < N ? i + k : 0] : 0u;
+    }
+}
+template <bool EVEN>
+__device__ __attribute__((always_inline)) inline void load16(const uint16_t* row, int c, int cols, uint32_t (&w)[8]) {
+  if (EVEN || cols - c >= 16) {
+    __builtin_memcpy(w, row + c, 32);
+  } else if (cols >= 16) {
+    const int gone = 16 - cols % 16;
+    __builtin_memcpy(w, row + (cols - 16), 32);
+    shift_down(w, gone >> 1);
+    if (gone & 1) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = (w[i] >> 16) | (i < 7 ? w[i < 7 ? i + 1 : 0] << 16 : 0u);
+    }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t lo = (2 * i < cnt) ? (uint32_t)p[2 * i] : 0u;
-      const uint32_t hi = (2 * i + 1 < cnt) ? (uint32_t)p[2 * i + 1] : 0u;
+      const uint32_t lo = (2 * i < cols) ? (uint32_t)row[2 * i] : 0u;
+      const uint32_t hi = (2 * i + 1 < cols) ? (uint32_t)row[2 * i + 1] : 0u;
       w[i] = lo | (hi << 16);
     }
   }
 }
+template <bool EVEN>
 __device__ __attribute__((always_inline)) inline void store16(uint16_t* p, int cnt, const uint32_t (&w)[8]) {
-  if (cnt >= 16) {
+  if (EVEN || cnt >= 16) {
     __builtin_memcpy(p, w, 32);
   } else {
 #pragma unroll
@@ -56,18 +79,25 @@ __device__ __attribute__((always_inline)) inline void store16(uint16_t* p, int c
   }
 }
 
-__device__ __attribute__((always_inline)) inline void load_weight(const NormArgs& a, int c, int cnt, float (&v)[16]) {
+template <bool EVEN>
+__device__ __attribute__((always_inline)) inline void load_weight(const NormArgs& a, int c, float (&v)[16]) {
   if (a.w_f32) {
-    const float* p = reinterpret_cast<const float*>(a.w) + c;
-    if (cnt >= 16) {
-      __builtin_memcpy(v, p, 64);
+    const float* p = reinterpret_cast<const float*>(a.w);
+    uint32_t w[16];
+    if (EVEN || a.cols - c >= 16) {
+      __builtin_memcpy(w, p + c, 64);
+    } else if (a.cols >= 16) {
+      __builtin_memcpy(w, p + (a.cols - 16), 64);
+      shift_down(w, 16 - a.cols % 16);
     } else {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = (i < cnt) ? p[i] : 0.0f;
+      for (int i = 0; i < 16; ++i) w[i] = (i < a.cols) ? f2u(p[i]) : 0u;
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = u2f(w[i]);
   } else {
     uint32_t w[8];
-    load16(reinterpret_cast<const uint16_t*>(a.w) + c, cnt, w);
+    load16<EVEN>(reinterpret_cast<const uint16_t*>(a.w), c, a.cols, w);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       v[2 * i] = bf16_lo(w[i]);
@@ -77,14 +107,17 @@ __device__ __attribute__((always_inline)) inline void load_weight(const NormArgs
 }
 
 // A unit of h; with a residual the sum, written to a.sum where the caller wants it.
-__device__ __attribute__((always_inline)) inline void load_h(const NormArgs& a, int64_t row, int c, int cnt, uint32_t (&h)[8]) {
-  load16(a.x + row * a.ldx + c, cnt, h);
+// (In place, a row's last unit may read elements that its neighbour has just replaced:
+// those that are shifted out.)
+template <bool EVEN>
+__device__ __attribute__((always_inline)) inline void load_h(const NormArgs& a, int64_t row, int c, uint32_t (&h)[8]) {
+  load16<EVEN>(a.x + row * a.ldx, c, a.cols, h);
   if (a.res) {
     uint32_t r[8];
-    load16(a.res + row * a.ldr + c, cnt, r);
+    load16<EVEN>(a.res + row * a.ldr, c, a.cols, r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) h[i] = pk_bf16(bf16_lo(h[i]) + bf16_lo(r[i]), bf16_hi(h[i]) + bf16_hi(r[i]));
-    if (a.sum) store16(a.sum + row * a.lds + c, cnt, h);
+    if (a.sum) store16<EVEN>(a.sum + row * a.lds + c, a.cols - c, h);
   }
 }
 
@@ -117,14 +150,14 @@ __device__ __attribute__((always_inline)) inline uint32_t amax16(const float (&y
 // Elements [c, c + 16) of row `row` of y, `cnt` of them in the row, in the output
 // format. s: tensor scale; r: its reciprocal (FP8). MX: the lanes of units 2 j and 2 j + 1
 // call this together. NVFP4 and MX rows are whole blocks.
-template <int FMT>
+template <int FMT, bool EVEN>
 __device__ __attribute__((always_inline)) inline void store_y(const NormArgs& a, int64_t row, int c, int cnt, const float (&y)[16],
                                                               float s, float r) {
   if constexpr (FMT == F_BF16) {
     uint32_t w[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = pk_bf16(y[2 * i], y[2 * i + 1]);
-    store16(reinterpret_cast<uint16_t*>(a.y) + row * a.ldy + c, cnt, w);
+    store16<EVEN>(reinterpret_cast<uint16_t*>(a.y) + row * a.ldy + c, cnt, w);
   } else if constexpr (FMT == F_FP8 || FMT == F_MXFP8) {
     if constexpr (FMT == F_MXFP8) {
       uint32_t am = amax16(y);
@@ -140,7 +173,7 @@ __device__ __attribute__((always_inline)) inline void store_y(const NormArgs& a,
       q[i] = hw_e4m3x4(t);
     }
     uint8_t* o = a.y + row * a.cols + c;
-    if (cnt >= 16) {
+    if (EVEN || cnt >= 16) {
       __builtin_memcpy(o, q, 16);
     } else {
 #pragma unroll
@@ -218,7 +251,7 @@ __device__ __attribute__((always_inline)) inline float scale_of_max(uint32_t m, 
 // 4096 84.7 (5.5 TB/s) against 91.1.
 //
 // Row `row` of thread t: h, and what its elements are multiplied by before the weight.
-template <int NV, int TPR>
+template <int NV, int TPR, bool EVEN>
 __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a, int64_t row, int t, float (&red)[2][16],
                                                                int& turn, uint32_t (&h)[NV][8], float& pre, float& rstd) {
   float ss = 0.0f;
@@ -227,7 +260,7 @@ __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a
     const int c = 16 * (t + TPR * i);
 #pragma unroll
     for (int j = 0; j < 8; ++j) h[i][j] = 0u;
-    if (c < a.cols) load_h(a, row, c, a.cols - c, h[i]);
+    if (c < a.cols) load_h<EVEN>(a, row, c, h[i]);
   }
 #pragma unroll
   for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, 1.0f);
@@ -246,7 +279,7 @@ __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a
 }
 
 // fn(first column, elements left in the row, the 16 values of y) for the thread's units.
-template <int NV, int TPR, class F>
+template <int NV, int TPR, bool EVEN, class F>
 __device__ __attribute__((always_inline)) inline void each_unit(const NormArgs& a, int t, const uint32_t (&h)[NV][8], float pre,
                                                                 float rstd, F fn) {
 #pragma unroll
@@ -254,7 +287,7 @@ __device__ __attribute__((always_inline)) inline void each_unit(const NormArgs& 
     const int c = 16 * (t + TPR * i);
     if (c >= a.cols) continue;
     float w[16], y[16];
-    load_weight(a, c, a.cols - c, w);
+    load_weight<EVEN>(a, c, w);
     norm16(h[i], w, pre, rstd, y);
     fn(c, a.cols - c, y);
   }
@@ -272,7 +305,7 @@ __device__ __attribute__((always_inline)) inline void leave_max(const NormArgs& 
     reinterpret_cast<uint32_t*>(a.y + j * a.region_bytes)[blockIdx.x] = am;
 }
 
-template <int FMT, int NV, int TPR>
+template <int FMT, int NV, int TPR, bool EVEN>
 __global__ void __launch_bounds__(TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs a) {
   __shared__ float red[2][16];
   const int t = (int)threadIdx.x % TPR, rpb = (int)blockDim.x / TPR;
@@ -286,10 +319,10 @@ __global__ void __launch_bounds__(TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs 
   for (int64_t row = (int64_t)blockIdx.x * rpb + threadIdx.x / TPR; row < a.rows; row += (int64_t)gridDim.x * rpb) {
     uint32_t h[NV][8];
     float pre, rstd;
-    norm_row<NV, TPR>(a, row, t, red, turn, h, pre, rstd);
-    each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
+    norm_row<NV, TPR, EVEN>(a, row, t, red, turn, h, pre, rstd);
+    each_unit<NV, TPR, EVEN>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
       if constexpr (FMT == F_AMAX) am = max(am, amax16(y));
-      else store_y<FMT>(a, row, c, cnt, y, s, r);
+      else store_y<FMT, EVEN>(a, row, c, cnt, y, s, r);
     });
   }
   if constexpr (FMT == F_AMAX) leave_max(a, am);
@@ -299,7 +332,7 @@ __global__ void __launch_bounds__(TPR == 1024 ? 1024 : 256) k_rms_norm(NormArgs 
 // one turn. SLOTS: from the maxima that the launch before left at the start of this
 // workgroup's codes (all read before the barrier that any code is written after);
 // otherwise the only workgroup's own, which holds every row of the tensor.
-template <int FMT, int NV, int TPR, bool SLOTS>
+template <int FMT, int NV, int TPR, bool SLOTS, bool EVEN>
 __global__ void __launch_bounds__(SLOTS && TPR < 1024 ? 256 : 1024) k_rms_norm_scaled(NormArgs a) {
   __shared__ float red[2][16];
   const int t = (int)threadIdx.x % TPR, rpb = (int)blockDim.x / TPR;
@@ -308,12 +341,12 @@ __global__ void __launch_bounds__(SLOTS && TPR < 1024 ? 256 : 1024) k_rms_norm_s
   uint32_t h[NV][8], am = 0;
   float pre = 1.0f, rstd = 0.0f;
   int turn = 0;
-  if (live) norm_row<NV, TPR>(a, row, t, red, turn, h, pre, rstd);
+  if (live) norm_row<NV, TPR, EVEN>(a, row, t, red, turn, h, pre, rstd);
   if constexpr (SLOTS) {
     const uint32_t* slots = reinterpret_cast<const uint32_t*>(a.y + (int64_t)blockIdx.x * a.region_bytes);
     for (int i = (int)threadIdx.x; i < a.slots; i += (int)blockDim.x) am = max(am, slots[i]);
   } else if (live) {
-    each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int, int, const float (&y)[16]) __attribute__((always_inline)) {
+    each_unit<NV, TPR, EVEN>(a, t, h, pre, rstd, [&](int, int, const float (&y)[16]) __attribute__((always_inline)) {
       am = max(am, amax16(y));
     });
   }
@@ -321,14 +354,14 @@ __global__ void __launch_bounds__(SLOTS && TPR < 1024 ? 256 : 1024) k_rms_norm_s
   const float r = (s > 0.0f) ? __fdiv_rn(1.0f, s) : 0.0f;
   if (blockIdx.x == 0 && threadIdx.x == 0) *a.tscale = s;
   if (!live) return;
-  each_unit<NV, TPR>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
-    store_y<FMT>(a, row, c, cnt, y, s, r);
+  each_unit<NV, TPR, EVEN>(a, t, h, pre, rstd, [&](int c, int cnt, const float (&y)[16]) __attribute__((always_inline)) {
+    store_y<FMT, EVEN>(a, row, c, cnt, y, s, r);
   });
 }
 
 // Rows too long for the registers: a workgroup walks the row twice (three times
 // where the squares overflow), the second time from the caches where it fits.
-template <int FMT>
+template <int FMT, bool EVEN>
 __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
   __shared__ float red[2][16];
   float s = 0.0f, r = 0.0f;
@@ -349,7 +382,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
     uint32_t h[8];
     float ss = 0.0f;
     for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
-      load_h(a, row, (int)c, (int)min((int64_t)16, a.cols - c), h);
+      load_h<EVEN>(a, row, (int)c, h);
       ss = squares(h, ss, 1.0f);
     }
     ss = row_sum<1024>(ss, red[turn]);
@@ -359,7 +392,7 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
       pre = kHugeScale;
       ss = 0.0f;
       for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
-        load_h(again, row, (int)c, (int)min((int64_t)16, a.cols - c), h);
+        load_h<EVEN>(again, row, (int)c, h);
         ss = squares(h, ss, pre);
       }
       rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, 0.0f);
@@ -368,11 +401,11 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
     for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
       const int cnt = (int)min((int64_t)16, a.cols - c);
       float w[16], y[16];
-      load_h(again, row, (int)c, cnt, h);
-      load_weight(a, (int)c, cnt, w);
+      load_h<EVEN>(again, row, (int)c, h);
+      load_weight<EVEN>(a, (int)c, w);
       norm16(h, w, pre, rstd, y);
       if constexpr (FMT == F_AMAX) am = max(am, amax16(y));
-      else store_y<FMT>(a, row, (int)c, cnt, y, s, r);
+      else store_y<FMT, EVEN>(a, row, (int)c, cnt, y, s, r);
     }
   }
   if constexpr (FMT == F_AMAX) leave_max(a, am);
@@ -441,23 +474,44 @@ static void with_plan(const NormPlan& p, F fn) {
   }
 }
 
-template <int FMT>
-static void launch_all(const NormArgs& a, const NormPlan& p, int64_t groups_max, hipStream_t st) {
-  const unsigned groups = (unsigned)std::min(p.groups, groups_max);
+// EVEN instances of every format, others of those that take any row length.
+template <int FMT, bool EVEN>
+static void launch_rows(const NormArgs& a, const NormPlan& p, unsigned groups, hipStream_t st) {
   if (p.tpr == 0) {
-    hipLaunchKernelGGL((k_rms_norm_long<FMT>), dim3(groups), dim3(1024), 0, st, a);
+    hipLaunchKernelGGL((k_rms_norm_long<FMT, EVEN>), dim3(groups), dim3(1024), 0, st, a);
     return;
   }
   with_plan(p, [&](auto NV, auto TPR) {
-    hipLaunchKernelGGL((k_rms_norm<FMT, NV(), TPR()>), dim3(groups), dim3((unsigned)(p.rpb * p.tpr)), 0, st, a);
+    hipLaunchKernelGGL((k_rms_norm<FMT, NV(), TPR(), EVEN>), dim3(groups), dim3((unsigned)(p.rpb * p.tpr)), 0, st, a);
   });
 }
+template <int FMT>
+static void launch_all(const NormArgs& a, const NormPlan& p, int64_t groups_max, hipStream_t st) {
+  const unsigned groups = (unsigned)std::min(p.groups, groups_max);
+  if constexpr (FMT == F_BF16 || FMT == F_FP8 || FMT == F_AMAX) {
+    if (a.cols % 16 != 0) {
+      launch_rows<FMT, false>(a, p, groups, st);
+      return;
+    }
+  }
+  launch_rows<FMT, true>(a, p, groups, st);
+}
 
+template <int FMT, bool SLOTS, bool EVEN>
+static void launch_scaled_rows(const NormArgs& a, const NormPlan& p, unsigned groups, unsigned threads, hipStream_t st) {
+  with_plan(p, [&](auto NV, auto TPR) {
+    hipLaunchKernelGGL((k_rms_norm_scaled<FMT, NV(), TPR(), SLOTS, EVEN>), dim3(groups), dim3(threads), 0, st, a);
+  });
+}
 template <int FMT, bool SLOTS>
 static void launch_scaled(const NormArgs& a, const NormPlan& p, unsigned groups, unsigned threads, hipStream_t st) {
-  with_plan(p, [&](auto NV, auto TPR) {
-    hipLaunchKernelGGL((k_rms_norm_scaled<FMT, NV(), TPR(), SLOTS>), dim3(groups), dim3(threads), 0, st, a);
-  });
+  if constexpr (FMT == F_FP8) {
+    if (a.cols % 16 != 0) {
+      launch_scaled_rows<FMT, SLOTS, false>(a, p, groups, threads, st);
+      return;
+    }
+  }
+  launch_scaled_rows<FMT, SLOTS, true>(a, p, groups, threads, st);
 }
 
 // Up to so many workgroups the maxima are left in every workgroup's codes: a launch
@@ -482,10 +536,12 @@ static hipError_t launch_dynamic(NormArgs a, hipStream_t st) {
     b.res = nullptr;
   }
   b.sum = nullptr;
-  if (p.tpr != 0 && p.groups <= std::min(kNormSlots, row_bytes / 4) && row_bytes % 4 == 0 &&
+  // (the last workgroup may have fewer rows, so fewer bytes of codes)
+  const int64_t region_bytes = p.rpb * row_bytes, last_bytes = (a.rows - (p.groups - 1) * p.rpb) * row_bytes;
+  if (p.tpr != 0 && p.groups <= std::min(kNormSlots, last_bytes / 4) && region_bytes % 4 == 0 &&
       reinterpret_cast<uintptr_t>(a.y) % 4 == 0) {
     a.regions = p.groups;
-    a.region_bytes = b.region_bytes = p.rpb * row_bytes;
+    a.region_bytes = b.region_bytes = region_bytes;
     b.slots = (int)p.groups;
     launch_all<F_AMAX>(a, p, p.groups, st);
     launch_scaled<FMT, true>(b, p, (unsigned)p.groups, (unsigned)(p.rpb * p.tpr), st);
