@@ -12,8 +12,10 @@
 // HBM-bound: x and the residual are read once, h and y written once. A row stays in
 // the registers of the threads that share it (packed bf16, 16 elements a unit: a whole
 // NVFP4 block, half an MX one, and a 16-byte store of FP8 codes), from the loads to the
-// codes. Rows of any alignment and length: whole units are loaded with wide loads
-// that need no alignment, a shorter last one element by element.
+// codes. Rows of any alignment and length: units are loaded with wide loads that
+// need no alignment, a shorter last one shifted into place (load16). Static FP8 with a
+// residual: 4608 x 3072 20.6 us (4.8 TB/s), 16384 x 4096 86 us (5.5 TB/s), 1 x 1024 2.6 us
+// (one launch's latency).
 //
 // A tensor scale taken from y (dynamic FP8, NVFP4) needs the largest |y| of all
 // rows before the first code: one workgroup does a tensor of few rows in one launch;
@@ -35,9 +37,10 @@ enum { F_BF16 = 0, F_FP8 = 1, F_NVFP4 = 2, F_MXFP4 = 3, F_MXFP8 = 4, F_AMAX = 5 
 // ---------------------------------------------------------------- 16 elements of a row
 // Elements [c, c + 16) of a row of cols, zero from cols on. EVEN: cols % 16 == 0, every
 // unit whole (an instance of its own: with the code for shorter units behind branches
-// the others take 10 % longer, 4608 x 3072 23.4 us, now 20.6). A row's last unit, if shorter, is loaded as the row's last 16 elements and shifted down, the same in every row: one
-// latency, where a condition on each element made 16 loads follow each other (a row of
-// fewer than 16 elements still takes them).
+// the others take 10 % longer, 4608 x 3072 23.4 us, now 20.6). A row's last unit, if
+// shorter, is loaded as the row's last 16 elements and shifted down, the same in every
+// row: one latency, where a condition on each element made 16 loads follow each other
+// (300 x 1001 5.1 us, now 4.6; a row of fewer than 16 elements still takes them).
 template <int N>  // words; down by `words` of them
 __device__ __attribute__((always_inline)) inline void shift_down(uint32_t (&w)[N], int words) {
 #pragma unroll
@@ -246,9 +249,9 @@ __device__ __attribute__((always_inline)) inline float scale_of_max(uint32_t m, 
 // TPR threads share a row, NV units of 16 elements each: unit t + TPR i. TPR <= 64: a
 // workgroup has blockDim / TPR rows at a time, else one. One or two units a thread
 // measured best at nearly every size (12 shapes from 1 x 1024 to 16384 x 4096, TPR 64 to
-// 1024, units of 8 and 16): static FP8 with a residual 4608 x 3072 22.7 us (4.4 TB/s)
-// with a workgroup per row against 25.3 with a wave, 500 x 3072 5.3 against 6.7, 16384 x
-// 4096 84.7 (5.5 TB/s) against 91.1.
+// 1024, units of 8 and 16; before the EVEN instances): static FP8 with a residual 4608 x
+// 3072 22.7 us with a workgroup per row against 25.3 with a wave, 500 x 3072 5.3 against
+// 6.7, 16384 x 4096 84.7 against 91.1. Non-temporal loads or stores lose 5 to 30 %.
 //
 // Row `row` of thread t: h, and what its elements are multiplied by before the weight.
 template <int NV, int TPR, bool EVEN>
