@@ -233,7 +233,8 @@ __device__ __attribute__((always_inline)) inline uint32_t group_max(uint32_t v) 
 }
 
 // Squares of elements past 2^64 leave fp32: such a row (a sum that is no finite
-// number) is summed again times 2^-96, an exact factor, which its elements get too.
+// number, or none with eps) is summed again times 2^-96, an exact factor, which its
+// elements get too, and eps its square.
 constexpr float kHugeScale = 1.262177448353618888658765e-29f;  // 2^-96
 
 __device__ __attribute__((always_inline)) inline float rstd_of(float ss, int cols, float eps) {
@@ -271,12 +272,12 @@ __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a
   turn ^= 1;
   pre = 1.0f;
   rstd = rstd_of(ss, a.cols, a.eps);
-  if (!(ss <= 3.40282347e38f)) {  // the same in every thread of the row
+  if (!(ss + a.eps <= 3.40282347e38f)) {  // the same in every thread of the row
     pre = kHugeScale;
     ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, pre);
-    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, 0.0f);
+    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale);
     turn ^= 1;
   }
 }
@@ -391,14 +392,14 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
     ss = row_sum<1024>(ss, red[turn]);
     turn ^= 1;
     float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
-    if (!(ss <= 3.40282347e38f)) {
+    if (!(ss + a.eps <= 3.40282347e38f)) {
       pre = kHugeScale;
       ss = 0.0f;
       for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
         load_h<EVEN>(again, row, (int)c, h);
         ss = squares(h, ss, pre);
       }
-      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, 0.0f);
+      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale);
       turn ^= 1;
     }
     for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {

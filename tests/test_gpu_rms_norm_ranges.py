@@ -1,0 +1,33 @@
+"""rms_norm where the squares leave fp32's range, against its formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_21849_amd as q
+from gpu_util import log
+from norm_util import bf16_tensor, check_norm, reference
+
+pytestmark = pytest.mark.gpu
+
+# lanes of a wave, a workgroup of 128, 256 (few and many rows) and 1024, a row walked twice; row ends inside a unit
+COLS = [48, 333, 2048, 4096, 5000, 12001, 20000, 49200]
+
+
+def _check(x, cols, eps, rng):
+    w = torch.from_numpy((1.0 + 0.2 * rng.standard_normal(cols)).astype(np.float32)).cuda()
+    for residual in (False, True):
+        for rows in (len(x), 300):
+            t = x.repeat(-(-rows // len(x)), 1)[:rows]
+            res = torch.zeros_like(t) if residual else None
+            _, y64 = reference(t, w, eps, res)
+            y = q.rms_norm(t, w, eps, residual=res)
+            check_norm(y if res is None else y[0], y64, q.QG_FMT_BF16)
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("eps", [1e34, 1e37, 3e38])
+def test_large_eps_beside_an_overflowing_sum(cols, eps):
+    log("rms_norm cols=%d eps=%g" % (cols, eps))
+    rng = np.random.default_rng(cols)
+    x = bf16_tensor(rng, 5, cols).float() * torch.tensor([[2.0 ** 58], [2.0 ** 61], [2.0 ** 63], [2.0 ** 70], [2.0 ** 120]], device="cuda")
+    _check(x.bfloat16(), cols, eps, rng)
