@@ -233,9 +233,11 @@ __device__ __attribute__((always_inline)) inline uint32_t group_max(uint32_t v) 
 }
 
 // Squares of elements past 2^64 leave fp32: such a row (a sum that is no finite
-// number, or none with eps) is summed again times 2^-96, an exact factor, which its
-// elements get too, and eps its square.
+// number, or none with eps) is summed again times 2^-96, an exact factor, and eps times
+// its square. Its elements get 2^-4 of the factor and r the rest (r is then at least
+// 2^-124, a normal number), so that elements far below the largest keep their digits.
 constexpr float kHugeScale = 1.262177448353618888658765e-29f;  // 2^-96
+constexpr float kHugePre = 0.0625f, kHugeRest = 2.0194839173657902e-28f;  // 2^-4, 2^-92
 
 __device__ __attribute__((always_inline)) inline float rstd_of(float ss, int cols, float eps) {
   const float v = __fadd_rn(__fdiv_rn(ss, (float)cols), eps);
@@ -273,11 +275,11 @@ __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a
   pre = 1.0f;
   rstd = rstd_of(ss, a.cols, a.eps);
   if (!(ss + a.eps <= 3.40282347e38f)) {  // the same in every thread of the row
-    pre = kHugeScale;
     ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, pre);
-    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale);
+    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, kHugeScale);
+    pre = kHugePre;
+    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale) * kHugeRest;
     turn ^= 1;
   }
 }
@@ -393,13 +395,13 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
     turn ^= 1;
     float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
     if (!(ss + a.eps <= 3.40282347e38f)) {
-      pre = kHugeScale;
       ss = 0.0f;
       for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
         load_h<EVEN>(again, row, (int)c, h);
-        ss = squares(h, ss, pre);
+        ss = squares(h, ss, kHugeScale);
       }
-      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale);
+      pre = kHugePre;
+      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale) * kHugeRest;
       turn ^= 1;
     }
     for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {

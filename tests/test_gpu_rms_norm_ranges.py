@@ -31,3 +31,13 @@ def test_large_eps_beside_an_overflowing_sum(cols, eps):
     rng = np.random.default_rng(cols)
     x = bf16_tensor(rng, 5, cols).float() * torch.tensor([[2.0 ** 58], [2.0 ** 61], [2.0 ** 63], [2.0 ** 70], [2.0 ** 120]], device="cuda")
     _check(x.bfloat16(), cols, eps, rng)
+
+
+@pytest.mark.parametrize("cols", COLS)
+def test_small_elements_of_an_overflowing_row(cols):
+    """One element past 2^64 and the rest far below it: those keep their digits."""
+    log("rms_norm cols=%d" % cols)
+    rng = np.random.default_rng(cols)
+    x = bf16_tensor(rng, 4, cols).float() * torch.tensor([[2.0 ** -20], [2.0 ** -35], [2.0 ** -40], [2.0 ** -45]], device="cuda")
+    x[:, cols // 3] = 2.0 ** 70
+    _check(x.bfloat16(), cols, 1e-6, rng)
