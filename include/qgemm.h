@@ -419,8 +419,9 @@ qg_status qg_gemm_fused(qg_format a_fmt, const void *a, const void *a_block_scal
  *   tensor_scale  out: FP8 and NVFP4 (else NULL).
  * Except where said, no two buffers overlap. Rows of any alignment and length
  * (any cols for bf16 and FP8; NVFP4 cols % 16 == 0, MX cols % 32 == 0, else
- * QG_ERR_SHAPE). Squares past fp32's range are summed scaled, so finite rows
- * give finite norms; a row holding inf or NaN gives NaN (bf16 output) or
+ * QG_ERR_SHAPE). Squares past fp32's range, or below it where eps does not
+ * hide them, are summed scaled, so that finite rows of any size give the
+ * formula's finite norms; a row holding inf or NaN gives NaN (bf16 output) or
  * unspecified codes, and the tensor scale NaN. An empty tensor gets
  * tensor_scale = 0.
  */

@@ -232,16 +232,33 @@ __device__ __attribute__((always_inline)) inline uint32_t group_max(uint32_t v) 
   return v;
 }
 
-// Squares of elements past 2^64 leave fp32: such a row (a sum that is no finite
-// number, or none with eps) is summed again times 2^-96, an exact factor, and eps times
-// its square. Its elements get 2^-4 of the factor and r the rest (r is then at least
-// 2^-124, a normal number), so that elements far below the largest keep their digits.
-constexpr float kHugeScale = 1.262177448353618888658765e-29f;  // 2^-96
-constexpr float kHugePre = 0.0625f, kHugeRest = 2.0194839173657902e-28f;  // 2^-4, 2^-92
+// Squares of elements past 2^64 leave fp32, and those below 2^-63 lose digits to its
+// subnormal numbers. A row whose sum is no finite number (or none with eps), or so small
+// that those count and eps does not hide them, is summed again times 2^-96 or 2^96, an
+// exact factor, and eps times its square. Small elements get the factor too. Large
+// ones get 2^-4 of it and r the rest (r is then at least 2^-124, a normal number), so
+// that elements far below the largest keep their digits.
+constexpr float kDown = 1.262177448353618888658765e-29f, kUp = 7.9228162514264337593543950336e28f;  // 2^-96, 2^96
+constexpr float kDownPre = 0.0625f, kDownRest = 2.0194839173657902e-28f;                          // 2^-4, 2^-92
+// A subnormal square's rounding is at most 2^-150: of all of a row less than 2^-119 (2^31
+// elements), 2^-39 of a sum of 2^-80; in their mean 2^-30 of an eps of 2^-120.
+constexpr float kSmallSum = 8.2718061255302767e-25f, kSmallEps = 7.5231638452626401e-37f;  // 2^-80, 2^-120
 
 __device__ __attribute__((always_inline)) inline float rstd_of(float ss, int cols, float eps) {
   const float v = __fadd_rn(__fdiv_rn(ss, (float)cols), eps);
   return v > 0.0f || v != v ? __fdiv_rn(1.0f, __fsqrt_rn(v)) : 0.0f;  // (a row of zeros with eps = 0)
+}
+
+// What the squares of a row of sum ss are summed again with; 1: they need not be. The
+// same in every thread of the row.
+__device__ __attribute__((always_inline)) inline float again_by(float ss, float eps) {
+  if (!(ss + eps <= 3.40282347e38f)) return kDown;
+  return ss < kSmallSum && eps < kSmallEps ? kUp : 1.0f;
+}
+// The factors of the elements, from the sum ss of the squares times f f.
+__device__ __attribute__((always_inline)) inline void factors_again(float ss, int cols, float eps, float f, float& pre, float& rstd) {
+  rstd = rstd_of(ss, cols, eps * f * f) * (f < 1.0f ? kDownRest : 1.0f);
+  pre = f < 1.0f ? kDownPre : f;
 }
 
 __device__ __attribute__((always_inline)) inline float scale_of_max(uint32_t m, float divisor) {
@@ -274,12 +291,12 @@ __device__ __attribute__((always_inline)) inline void norm_row(const NormArgs& a
   turn ^= 1;
   pre = 1.0f;
   rstd = rstd_of(ss, a.cols, a.eps);
-  if (!(ss + a.eps <= 3.40282347e38f)) {  // the same in every thread of the row
+  const float f = again_by(ss, a.eps);
+  if (f != 1.0f) {
     ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, kHugeScale);
-    pre = kHugePre;
-    rstd = rstd_of(row_sum<TPR>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale) * kHugeRest;
+    for (int i = 0; i < NV; ++i) ss = squares(h[i], ss, f);
+    factors_again(row_sum<TPR>(ss, red[turn]), a.cols, a.eps, f, pre, rstd);
     turn ^= 1;
   }
 }
@@ -366,7 +383,7 @@ __global__ void __launch_bounds__(SLOTS && TPR < 1024 ? 256 : 1024) k_rms_norm_s
 }
 
 // Rows too long for the registers: a workgroup walks the row twice (three times
-// where the squares overflow), the second time from the caches where it fits.
+// where the squares leave fp32), the second time from the caches where it fits.
 template <int FMT, bool EVEN>
 __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
   __shared__ float red[2][16];
@@ -394,14 +411,14 @@ __global__ void __launch_bounds__(1024) k_rms_norm_long(NormArgs a) {
     ss = row_sum<1024>(ss, red[turn]);
     turn ^= 1;
     float pre = 1.0f, rstd = rstd_of(ss, a.cols, a.eps);
-    if (!(ss + a.eps <= 3.40282347e38f)) {
+    const float f = again_by(ss, a.eps);
+    if (f != 1.0f) {
       ss = 0.0f;
       for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {
         load_h<EVEN>(again, row, (int)c, h);
-        ss = squares(h, ss, kHugeScale);
+        ss = squares(h, ss, f);
       }
-      pre = kHugePre;
-      rstd = rstd_of(row_sum<1024>(ss, red[turn]), a.cols, a.eps * kHugeScale * kHugeScale) * kHugeRest;
+      factors_again(row_sum<1024>(ss, red[turn]), a.cols, a.eps, f, pre, rstd);
       turn ^= 1;
     }
     for (int64_t c = 16 * (int64_t)threadIdx.x; c < a.cols; c += 16 * 1024) {

@@ -41,3 +41,24 @@ def test_small_elements_of_an_overflowing_row(cols):
     x = bf16_tensor(rng, 4, cols).float() * torch.tensor([[2.0 ** -20], [2.0 ** -35], [2.0 ** -40], [2.0 ** -45]], device="cuda")
     x[:, cols // 3] = 2.0 ** 70
     _check(x.bfloat16(), cols, 1e-6, rng)
+
+
+@pytest.mark.parametrize("cols", COLS)
+@pytest.mark.parametrize("eps", [0.0, 1e-45, 1e-40, 1e-37, 1e-35])
+def test_squares_below_the_smallest_number(cols, eps):
+    """Rows whose squares are subnormal or zero, where eps does not hide them."""
+    log("rms_norm cols=%d eps=%g" % (cols, eps))
+    rng = np.random.default_rng(cols)
+    x = bf16_tensor(rng, 7, cols).float() * torch.tensor([[1e-12], [1e-17], [1e-20], [1e-22], [1e-30], [1e-38], [0.0]], device="cuda")
+    x[6, cols // 2] = 2.0 ** -133  # the smallest bf16
+    _check(x.bfloat16(), cols, eps, rng)
+
+
+@pytest.mark.parametrize("cols", COLS)
+def test_squares_below_the_smallest_number_quantized(cols):
+    rng = np.random.default_rng(cols)
+    cols = cols // 32 * 32
+    x, w = (1e-30 * bf16_tensor(rng, 20, cols).float()).bfloat16(), torch.ones(cols, device="cuda")
+    _, y64 = reference(x, w, 0.0)
+    for fmt in (q.QG_FMT_FP8_E4M3, q.QG_FMT_NVFP4, q.QG_FMT_MXFP4, q.QG_FMT_MXFP8):
+        check_norm(q.rms_norm(x, w, 0.0, fmt=fmt), y64, fmt)
