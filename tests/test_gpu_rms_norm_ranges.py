@@ -1,4 +1,5 @@
-"""rms_norm where the squares leave fp32's range, against its formula in 64 bits."""
+"""rms_norm where the squares leave fp32's range, upwards and downwards, against its
+formula in 64 bits, and that a row's norm does not depend on the rows beside it."""
 import numpy as np
 import pytest
 import torch
@@ -62,3 +63,18 @@ def test_squares_below_the_smallest_number_quantized(cols):
     _, y64 = reference(x, w, 0.0)
     for fmt in (q.QG_FMT_FP8_E4M3, q.QG_FMT_NVFP4, q.QG_FMT_MXFP4, q.QG_FMT_MXFP8):
         check_norm(q.rms_norm(x, w, 0.0, fmt=fmt), y64, fmt)
+
+
+@pytest.mark.parametrize("cols", [40, 1024, 3001, 4096, 4112, 5003, 6144, 9216, 12305, 16384, 20000])
+def test_a_row_among_any_number_of_rows(cols):
+    """The sum's order is fixed by cols: the same bits in calls of 1024, 257, 256 and one row."""
+    log("rms_norm rows of cols=%d" % cols)
+    rng = np.random.default_rng(cols)
+    x = bf16_tensor(rng, 1024, cols)
+    w = torch.from_numpy((1.0 + 0.2 * rng.standard_normal(cols)).astype(np.float32)).cuda()
+    y = q.rms_norm(x, w)
+    for part in (256, 257):
+        for i in range(0, 1024, part):
+            assert torch.equal(q.rms_norm(x[i:i + part], w), y[i:i + part])
+    for i in (0, 511, 1023):
+        assert torch.equal(q.rms_norm(x[i:i + 1], w), y[i:i + 1])
