@@ -563,6 +563,12 @@ def _dtype_code(t, name: str) -> int:
     return QG_OUT_F32 if t.dtype == torch.float32 else QG_OUT_BF16
 
 
+def _enumerator(v: int, known: tuple, where: str) -> None:
+    """Refuse v as the library would; ctypes passes it on modulo 2^32."""
+    if v not in known:
+        raise QGError(1, where)
+
+
 def _pitch(t) -> int:
     """Elements between the rows of a 2-D tensor (a size-1 dimension may carry any stride)."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
@@ -585,6 +591,7 @@ def _linear_epilogue(a, w_packed, w_fmt, n, bias, act, residual, gated, out_dtyp
     import torch
     m, k, a_fmt, a_data, a_bs, a_ts, lda, dev = _operands(a, w_packed)
     _current_device(dev)
+    _enumerator(act, (QG_ACT_NONE, QG_ACT_SILU, QG_ACT_GELU_TANH, QG_ACT_GELU_ERF), "qg_gemm_fused")
     if out_dtype not in (QG_OUT_BF16, QG_OUT_F32, QG_OUT_FP8, QG_OUT_NVFP4):
         raise ValueError("out_dtype must be QG_OUT_BF16, QG_OUT_F32, QG_OUT_FP8 or QG_OUT_NVFP4")
     e = Epilogue(act=act, gated=1 if gated else 0)
@@ -683,6 +690,7 @@ def rms_norm(x, weight, eps: float = 1e-6, residual=None, fmt: int = QG_FMT_BF16
     rows, cols = x.shape
     dev = x.device
     _current_device(dev)
+    _enumerator(fmt, (QG_FMT_BF16, QG_FMT_FP8_E4M3, QG_FMT_NVFP4, *MX_FORMATS), "qg_rms_norm")
     wdt = _dtype_code(weight, "weight")
     _need(weight, "weight", weight.dtype, (cols,), dev)
     h = None
