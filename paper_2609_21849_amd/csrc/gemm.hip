@@ -552,6 +552,7 @@ __device__ __attribute__((always_inline)) inline void finish_wide(const GemmArgs
       together(bias[k]);
     }
   }
+  static_assert(RES == 0 || W * RSZ % 16 == 0, "16-byte loads");
   uint32_t res[ITS][RES == 2 ? W : W / 2];
   auto inside = [&](int i, int j, int it) __attribute__((always_inline)) {
     return i + it * B::STEP_ROWS < rows && j + it * B::STEP_COLS < cols;
@@ -561,19 +562,13 @@ __device__ __attribute__((always_inline)) inline void finish_wide(const GemmArgs
 #pragma unroll
     for (int it = 0; it < ITS; ++it) {
       const uint32_t off = inside(i, j, it) ? (uint32_t)(res0 + (it * B::STEP_ROWS * ldr + it * B::STEP_COLS) * RSZ) : OOB;
-      if constexpr (W * RSZ == 8) {
-        const v2i t = __builtin_amdgcn_raw_buffer_load_b64(rs_r, off, so, 0);
-        res[it][0] = (uint32_t)t.x;
-        res[it][1] = (uint32_t)t.y;
-      } else {
 #pragma unroll
-        for (int h = 0; h < W * RSZ / 16; ++h) {
-          const v4i t = __builtin_amdgcn_raw_buffer_load_b128(rs_r, off + 16 * h, so, 0);
-          res[it][4 * h] = (uint32_t)t.x;
-          res[it][4 * h + 1] = (uint32_t)t.y;
-          res[it][4 * h + 2] = (uint32_t)t.z;
-          res[it][4 * h + 3] = (uint32_t)t.w;
-        }
+      for (int h = 0; h < W * RSZ / 16; ++h) {
+        const v4i t = __builtin_amdgcn_raw_buffer_load_b128(rs_r, off + 16 * h, so, 0);
+        res[it][4 * h] = (uint32_t)t.x;
+        res[it][4 * h + 1] = (uint32_t)t.y;
+        res[it][4 * h + 2] = (uint32_t)t.z;
+        res[it][4 * h + 3] = (uint32_t)t.w;
       }
     }
   };
