@@ -203,17 +203,21 @@ __device__ __attribute__((always_inline)) inline void store_nv_quad(const GemmAr
 #if QG_EPILOGUE
 // ---------------------------------------------------------------- bias, activation, residual, gate
 // y = act(z + bias) + residual, or act(z_gate + bias) (z_up + bias) (kGated: weight rows, and so
-// accumulator columns, 2 i and 2 i + 1 are output i's gate and up rows), z the sum times the tensor scales: every step in fp32, one
-// rounding at the store. The exponential is the hardware's 2^x of z log2 e: its
-// argument's rounding leaves a relative error of |z| 2^-24, below the bf16 and FP8
-// outputs' half steps for any |z| with a nonzero result.
+// accumulator columns, 2 i and 2 i + 1 are output i's gate and up rows), z the sum times the
+// tensor scales: every step in fp32, one rounding at the store. The exponential is the
+// hardware's 2^x of z log2 e, whose rounding leaves a relative error of up to |z| 2^-24:
+// below the bf16 and FP8 outputs' half steps for any |z| with a nonzero result, and in
+// fp32 outputs, at far negative z, what qgemm.h allows for (SiLU 9 units of 2^-24 at -10, 33
+// at -40, 65 at -80). A second term of the argument would take two more operations a value.
 //   SiLU       z / (1 + e^-z)
 //   GELU tanh  z / (1 + e^-2u), u = sqrt(2 / pi) (z + 0.044715 z^3): 0.5 (1 + tanh u) is
 //              the logistic function of 2 u
 //   GELU erf   z Phi(z), Phi(-x) = exp(-x^2 / 2) t P(t), t = 1 / (1 + 0.3 x / sqrt 2), x >= 0: the
-//              scaled tail erfcx / 2 as a polynomial of degree 8 in t without a constant
-//              term, least in its largest relative error (2e-8; fitted by reweighted
-//              least squares over x / sqrt 2 in [0, 9.5]); no cancellation at z < 0
+//              scaled tail erfcx / 2 as t times a polynomial in t (the form of Hastings'
+//              approximations, Abramowitz and Stegun 7.1.26), here of degree 8 and fitted
+//              by reweighted least squares over x / sqrt 2 in [0, 9.5] to the least relative
+//              error (3.0e-8 with these constants; past 9.5 y is below 2^-100); no
+//              cancellation at z < 0
 // Far negative z: the exponential is inf, its reciprocal 0, the result -0.
 
 // The values in registers here, all at once: what makes them is not moved past this
@@ -509,7 +513,8 @@ struct Blocks16 {  // 16 x 16 MFMA tiles, the six of a wave's 96 columns at a ti
 // none, 1 bf16, 2 fp32). Its own cost in a tile of 256 x 256 outputs, against the plain
 // epilogue: nothing to add 1 us, SiLU and GELU 4 to 8 us (a quarter-rate exponential and
 // reciprocal a value: 52 cycles of a SIMD for 64 tanh-GELUs), half of that when gated,
-// a residual its bytes. Straight from the loop over pieces with a branch for each
+// a residual its bytes (twice their time where every tile ends in one round: FP8 4608 x
+// 3072 x 9216 99 to 102 us, plain 91). Straight from the loop over pieces with a branch for each
 // choice: FP8 4608 x 18432 x 3072 246 us, now 198 (plain 197), tanh-GELU and bias 276, now
 // 216, residual 319, now 243 (its 170 MB more to read: 27 us).
 template <class B, int OUT, int RES, int NI, int NJ, class Put>

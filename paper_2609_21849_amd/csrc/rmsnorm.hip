@@ -15,8 +15,9 @@
 // NVFP4 block, half an MX one, and a 16-byte store of FP8 codes), from the loads to the
 // codes. Rows of any alignment and length: units are loaded with wide loads that
 // need no alignment, a shorter last one shifted into place (load16). Static FP8 with a
-// residual: 4608 x 3072 20.6 us (4.8 TB/s), 16384 x 4096 86 us (5.5 TB/s), 1 x 1024 2.6 us
-// (one launch's latency).
+// residual, inputs in turn past the memory-side cache: 4608 x 3072 21.1 us (4.7 TB/s),
+// 16384 x 4096 85 us (5.5 TB/s), 1 x 1024 2.6 us (one launch's latency); of three inputs
+// in turn 4608 x 3072 18.4 (5.4 TB/s).
 //
 // A tensor scale taken from y (dynamic FP8, NVFP4) needs the largest |y| of all
 // rows before the first code: one workgroup does a tensor of few rows in one launch;
@@ -38,10 +39,10 @@ enum { F_BF16 = 0, F_FP8 = 1, F_NVFP4 = 2, F_MXFP4 = 3, F_MXFP8 = 4, F_AMAX = 5 
 // ---------------------------------------------------------------- 16 elements of a row
 // Elements [c, c + 16) of a row of cols, zero from cols on. EVEN: cols % 16 == 0, every
 // unit whole (an instance of its own: with the code for shorter units behind branches
-// the others take 10 % longer, 4608 x 3072 23.4 us, now 20.6). A row's last unit, if
+// the others take 10 % longer, 4608 x 3072 23.4 us against 20.6). A row's last unit, if
 // shorter, is loaded as the row's last 16 elements and shifted down, the same in every
 // row: one latency, where a condition on each element made 16 loads follow each other
-// (300 x 1001 5.1 us, now 4.6; a row of fewer than 16 elements still takes them).
+// (300 x 1001 5.1 us against 4.6; a row of fewer than 16 elements still takes them).
 template <int N>  // words; down by `words` of them
 __device__ __attribute__((always_inline)) inline void shift_down(uint32_t (&w)[N], int words) {
 #pragma unroll
